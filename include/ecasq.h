@@ -374,6 +374,156 @@ ecasq_status ecasq_solve_batched(const void *x, ecasq_dtype dt, int64_t n, int64
                                  void *stream, double *codebooks, int32_t *t_out,
                                  ecasq_info *infos_dev);
 
+/*
+ * Products with 4-bit weights.  A weight matrix W of n_out x n_in is held as the
+ * symbols of one codebook of t <= 16 values (ecasq_solve and ecasq_quantize on
+ * the scaled weights) and a scale for every `group` consecutive inputs of a
+ * row:
+ *   W[o][i] = scales[o][i / group] * c[symbols[o][i]],
+ *   y[r][o] = sum_g scales[o][g] sum_{i in g} c[symbols[o][i]] x[r][i].
+ * The codebook values and the scales are held in dt (ECASQ_F16 or ECASQ_BF16),
+ * the type of x and y; products are exact, sums are kept in fp32 (a group's
+ * first, then the groups'), y is rounded once.
+ *
+ * ecasq_weights_size: bytes of the packed matrix (0 unless 1 <= n_out, n_in <=
+ * 2^24, n_out n_in <= 2^40 and group is a positive multiple of 32 up to 2^24; a
+ * group of n_in or more is one scale per row).
+ * ecasq_weights_pack lays a matrix out once for all products: symbols, device,
+ * n_out x n_in bytes (a symbol of t or more counts as t-1); codebook, device, t
+ * fp64 values, each rounded to dt once; scales, device, n_out x ceil(n_in /
+ * group) of dt; packed, device, at least ecasq_weights_size bytes (checked
+ * against packed_bytes), 16-byte aligned.
+ * ecasq_matvec: x, device, m rows of n_in entries x_stride >= n_in entries
+ * apart, 1 <= m <= 2^20; y, device, m x n_out.  x and y need the alignment of
+ * their type only.  The packed matrix is read once for every 64 rows of x.  No
+ * workspace; results do not depend on the run or on m's other rows.  Both return
+ * once the work is enqueued.
+ */
+size_t ecasq_weights_size(int64_t n_out, int64_t n_in, int64_t group);
+ecasq_status ecasq_weights_pack(const uint8_t *symbols, const double *codebook, int32_t t,
+                                const void *scales, ecasq_dtype dt, int64_t n_out, int64_t n_in,
+                                int64_t group, void *stream, void *packed, size_t packed_bytes);
+ecasq_status ecasq_matvec(const void *packed, ecasq_dtype dt, int64_t n_out, int64_t n_in,
+                          int64_t group, const void *x, int64_t m, int64_t x_stride,
+                          void *stream, void *y);
+
+/*
+ * A paged key/value cache.  Each sequence's rows lie in pages of page_size
+ * slots; table[b][i] is the page of its slots i page_size and up.  A page holds
+ * its rows head by head:
+ *   coded = 0: k, v [n_pages][heads][page_size][head_dim] of dt;
+ *   coded = 1: k, v [n_pages][heads][page_size][head_dim / 2] bytes, byte i
+ *     holding the symbols of entries 2i (low four bits) and 2i+1, and k_books,
+ *     v_books [n_pages][heads][page_size][16] of dt, each row's own codebook
+ *     (ecasq_solve_batched): 4 + 256 / head_dim bits an entry.
+ * dt is ECASQ_F16 or ECASQ_BF16; head_dim 64, 128 or 256; page_size a multiple
+ * of 16, 16 to 65536; 1 <= heads <= 1024; 1 <= batch <= 65535; k, v and the
+ * books are 16-byte aligned.  lens[b] is the number of slots of sequence b in
+ * use; a number below 0 counts as 0, one above max_pages page_size as that.  The
+ * slots of a table entry outside [0, n_pages) hold nothing: they are not read,
+ * not written, and get no weight.  A page with slots that a call writes must
+ * stand in one place of the table only; a page that is only read may be shared.
+ *
+ * mass and pos ([batch][heads][max_pages page_size], may be NULL where an entry
+ * point does not need them) hold for each slot the attention weight that it has
+ * gathered and the position of the token in it.  Attention does not depend on the
+ * order of the slots, so eviction moves rows into freed slots instead of
+ * shifting the cache, and pos tells how recent they are.
+ */
+typedef struct {
+    int32_t dt;        /* ecasq_dtype */
+    int32_t coded;     /* 0: rows of dt; 1: 4-bit symbols and a codebook per row */
+    int32_t heads;     /* key/value heads */
+    int32_t head_dim;
+    int32_t page_size; /* slots per page */
+    int32_t batch;     /* sequences */
+    int32_t max_pages; /* table entries per sequence */
+    int32_t n_pages;   /* pages that k and v hold */
+    void *k, *v;
+    void *k_books, *v_books; /* coded only */
+    const int32_t *table;    /* batch x max_pages */
+    const int32_t *lens;     /* batch */
+    float *mass;
+    int32_t *pos;
+} ecasq_kv_cache;
+
+/*
+ * New rows into the cache.  starts (device, batch + 1, ascending from 0): rows
+ * starts[b] .. starts[b+1]-1 are sequence b's new tokens, and lens already counts
+ * them: row i goes to slot lens[b] - starts[b+1] + i (advance lens first; a
+ * slot below 0 or past the table, or a row that no sequence has, is left out).
+ * new_k, new_v: device, `rows` tokens of heads x head_dim entries of dt, k_stride
+ * and v_stride (>= heads head_dim) entries apart, of their type's alignment.
+ * With c->mass, the slot's weight becomes 0; with c->pos, its position becomes
+ * positions[i], or the slot itself where positions is NULL.
+ *
+ * A coded cache takes each row's codebook as ecasq_solve_batched returns it for
+ * the rows of the same tokens (row r = token heads + head): k_codebooks, device,
+ * rows heads x s fp64, 2 <= s <= 32, and k_counts, device, rows heads int32, at
+ * most 16; the same for v.  The values are rounded to dt (they are exact where
+ * the codebook was solved on rows of dt) and entry e = r head_dim + j is
+ * rounded as ecasq_quantize rounds, its uniform from counter (h mod 2^32, h /
+ * 2^32, w, 0), h = e / 2, w = 2 for keys and 3 for values.  A row with a count
+ * outside 1 .. 16 (0 marks a row with NaN or Inf) is stored as NaN.  k_hat, v_hat
+ * (device, rows x heads x head_dim of dt, both or neither) receive the rows as
+ * they will be read, so that a prompt can be computed with them; rows that are
+ * left out are not written.  For coded = 0 the last eight arguments are ignored
+ * but for k_hat and v_hat, which must be NULL.  Returns once the work is
+ * enqueued.
+ */
+ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t k_stride,
+                            const void *new_v, int64_t v_stride, int64_t rows,
+                            const int32_t *starts, const int32_t *positions, void *stream,
+                            const double *k_codebooks, const int32_t *k_counts,
+                            const double *v_codebooks, const int32_t *v_counts, int32_t s,
+                            uint64_t seed, void *k_hat, void *v_hat);
+
+/*
+ * Attention of one new token of every sequence over its cache:
+ *   out[b][h] = sum_t p_t V[b][g][t],  p = softmax over the slots t < lens[b] of
+ *   scale q[b][h] . K[b][g][t],  g = h heads / q_heads;
+ * q: device, batch rows of q_heads x head_dim entries of dt, q_stride >= q_heads
+ * head_dim entries apart, of their type's alignment; q_heads a multiple of heads,
+ * at most 64 heads; out: device, batch x q_heads x head_dim of dt, 16-byte
+ * aligned.  Scores, weights and sums are fp32; out is rounded once.  A sequence
+ * with no slots to read, or whose scores are all -inf, gives zeros.  A NaN or
+ * infinity in a row that is read reaches the result; what lies in slots past
+ * lens[b] does not.
+ * mass_out (device, as c->mass; NULL: no weights): for each slot below lens[b]
+ * and head g, c->mass (0 where that is NULL) plus p_t summed over g's query heads
+ * in order; slots past lens[b] are left as they are.  mass_out may be c->mass.
+ * The length is split over workgroups and joined where batch and heads alone do
+ * not fill the card; results are the same bit for bit from run to run.
+ * workspace: at least ecasq_kv_attention_workspace bytes (0 for a bad cache or
+ * q_heads), 256-byte aligned, its contents of no meaning between calls; calls that
+ * overlap need one each.  Returns once the work is enqueued.
+ */
+size_t ecasq_kv_attention_workspace(const ecasq_kv_cache *c, int32_t q_heads, int32_t with_mass);
+ecasq_status ecasq_kv_attention(const ecasq_kv_cache *c, const void *q, int64_t q_stride,
+                                int32_t q_heads, double scale, float *mass_out, void *stream,
+                                void *out, void *workspace, size_t workspace_bytes);
+
+/*
+ * Eviction: every head of a sequence with lens[b] > keep gives up all but keep
+ * slots.  Kept are the slots with pos > (the largest pos of the head's slots) -
+ * recent, then those of the largest mass; ties, and any surplus among the first,
+ * go to the lowest slot (a NaN mass is below all others).  The i-th kept slot at
+ * or above keep, in ascending order, moves into the i-th freed slot below keep:
+ * its row of keys and values, its mass and its pos; other rows stay where they
+ * are, and slots at or above keep may be given to another sequence after the
+ * call.  mass_out, pos_out (as c->mass and c->pos, which are needed) receive the
+ * slots below min(lens[b], keep), lens_out (batch) that number; they may be
+ * c->mass, c->pos and c->lens.  keep >= 1, 0 <= recent <= keep.  Slots without
+ * a page are ranked and moved like others but have no rows (a row moved from one
+ * leaves the freed slot's row as it was).
+ * workspace: ecasq_kv_evict_workspace bytes (0 for a bad cache or keep), 256-byte
+ * aligned, as above.  Returns once the work is enqueued.
+ */
+size_t ecasq_kv_evict_workspace(const ecasq_kv_cache *c, int32_t keep);
+ecasq_status ecasq_kv_evict(const ecasq_kv_cache *c, int32_t keep, int32_t recent,
+                            float *mass_out, int32_t *pos_out, int32_t *lens_out, void *stream,
+                            void *workspace, size_t workspace_bytes);
+
 /* Bytes of device workspace a single-vector solve of d entries with at most s
  * values needs; flags: 1 = stored argmins (recovery 1 of schedule 0),
  * 2 = the tables of schedule 1, 4 = a permissible grid (alphabet 1 or 2)

@@ -15,7 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libecasq.so")
 SOURCES = ["prep.hip", "alphabet.hip", "dp.hip", "sweep.hip", "layers.hip", "held.hip", "opt.hip", "post.hip",
-           "rans.hip", "batched.hip", "search.hip", "api.cpp"]
+           "rans.hip", "batched.hip", "search.hip", "matvec.hip", "kvcache.hip", "kvattn.hip",
+           "api.cpp", "serve.cpp"]
 ARCH = os.environ.get("ECASQ_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -65,6 +65,27 @@ class ecasq_info(ctypes.Structure):
         return d
 
 
+class _kv_struct(ctypes.Structure):
+    _fields_ = [
+        ("dt", ctypes.c_int32),
+        ("coded", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_books", ctypes.c_void_p),
+        ("v_books", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p),
+        ("mass", ctypes.c_void_p),
+        ("pos", ctypes.c_void_p),
+    ]
+
+
 class EcasqError(RuntimeError):
     def __init__(self, status):
         self.status = status
@@ -80,6 +101,9 @@ EXPORTS = (
     "ecasq_solve_timeshare", "ecasq_quantize_timeshare", "ecasq_encode_bound", "ecasq_encode",
     "ecasq_decode", "ecasq_quantize_noalloc", "ecasq_inspect_enable", "ecasq_inspect_points",
     "ecasq_inspect_results", "ecasq_trim",
+    "ecasq_weights_size", "ecasq_weights_pack", "ecasq_matvec", "ecasq_kv_write",
+    "ecasq_kv_attention_workspace", "ecasq_kv_attention", "ecasq_kv_evict_workspace",
+    "ecasq_kv_evict",
 )
 
 
@@ -137,6 +161,23 @@ def lib():
     L.ecasq_timing_enable.restype = None
     L.ecasq_timing_read.argtypes = [i32, P(dbl), P(i64), P(i64), i32]
     L.ecasq_timing_read.restype = None
+    L.ecasq_weights_size.argtypes = [i64, i64, i64]
+    L.ecasq_weights_size.restype = ctypes.c_size_t
+    L.ecasq_weights_pack.argtypes = [vp, vp, i32, vp, i32, i64, i64, i64, vp, vp,
+                                     ctypes.c_size_t]
+    L.ecasq_matvec.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp]
+    L.ecasq_kv_write.argtypes = [P(_kv_struct), vp, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp,
+                                 i32, ctypes.c_uint64, vp, vp]
+    L.ecasq_kv_attention_workspace.argtypes = [P(_kv_struct), i32, i32]
+    L.ecasq_kv_attention_workspace.restype = ctypes.c_size_t
+    L.ecasq_kv_attention.argtypes = [P(_kv_struct), vp, i64, i32, dbl, vp, vp, vp, vp,
+                                     ctypes.c_size_t]
+    L.ecasq_kv_evict_workspace.argtypes = [P(_kv_struct), i32]
+    L.ecasq_kv_evict_workspace.restype = ctypes.c_size_t
+    L.ecasq_kv_evict.argtypes = [P(_kv_struct), i32, i32, vp, vp, vp, vp, vp, ctypes.c_size_t]
+    for name in ("ecasq_weights_pack", "ecasq_matvec", "ecasq_kv_write", "ecasq_kv_attention",
+                 "ecasq_kv_evict"):
+        getattr(L, name).restype = i32
     for name in ("ecasq_solve", "ecasq_solve_ex", "ecasq_solve_lagrangian", "ecasq_quantize",
                  "ecasq_solve_batched", "ecasq_histogram", "ecasq_dp_trace",
                  "ecasq_solve_budgets", "ecasq_solve_optimal", "ecasq_opt_trace",
@@ -399,6 +440,281 @@ def ecasq_solve_batched(x, s, bits_per_entry, options=None, stream=None):
                                    _ptr(cbs), _ptr(tt), _ptr(infos))
     _raise(st, (ECASQ_OK, ECASQ_EINFEASIBLE))
     return cbs, tt, infos
+
+
+# ---------------------------------------------------------------------------
+# Serving: products with 4-bit weights and the paged key/value cache.  These calls
+# run on their tensors' device, on its current stream or on `stream`, and allocate
+# what they return and their workspace there with torch's allocator.
+
+_HALF = {torch.float16: 1, torch.bfloat16: 2}
+
+
+class _on:
+    """The device of a call's tensors as the current one, and the call's stream
+    as torch's, so that what the call allocates belongs to that stream."""
+
+    def __init__(self, device, stream):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream must be on {device}")
+        self.was = None
+        if torch.cuda.current_device() != device.index:
+            self.was = torch.cuda.device(device)
+            self.was.__enter__()
+        self.stream = None
+        if stream is not None:
+            self.stream = torch.cuda.stream(stream)
+            self.stream.__enter__()
+        self.ptr = torch.cuda.current_stream().cuda_stream
+
+    def __enter__(self):
+        return self.ptr
+
+    def __exit__(self, *exc):
+        if self.stream is not None:
+            self.stream.__exit__(*exc)
+        if self.was is not None:
+            self.was.__exit__(*exc)
+
+
+def _tensor(x, name, dtype, device, shape=None):
+    """x, once it is seen to be a contiguous tensor as the library needs it."""
+    if not isinstance(x, torch.Tensor) or x.dtype != dtype or x.device != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on {device}")
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}")
+    if not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return x
+
+
+def _half_tensor(x, name):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in _HALF:
+        raise TypeError(f"{name} must be a float16 or bfloat16 CUDA (HIP) tensor")
+    return x
+
+
+def _rows_apart(x, inner):
+    """x as rows of `inner` entries and the entries between their starts; copied
+    where they do not lie that way."""
+    x = x.reshape(-1, inner) if x.is_contiguous() else x
+    flat, want = x.shape[0] if x.dim() else 1, 1
+    for size, step in zip(reversed(x.shape[1:]), reversed(x.stride()[1:])):
+        if size != 1 and step != want:
+            return x.contiguous(), inner
+        want *= size
+    step = x.stride(0) if flat > 1 else inner
+    return (x, step) if step >= inner else (x.contiguous(), inner)
+
+
+class ecasq_weights:
+    """A packed 4-bit weight matrix (ecasq_weights_pack)."""
+
+    __slots__ = ("packed", "dtype", "n_out", "n_in", "group")
+
+    def __init__(self, packed, dtype, n_out, n_in, group):
+        self.packed, self.dtype = packed, dtype
+        self.n_out, self.n_in, self.group = n_out, n_in, group
+
+
+def ecasq_weights_pack(symbols, codebook, scales, group, stream=None):
+    """Lays out symbols uint8 [n_out, n_in] with a codebook of at most 16 values
+    and scales (float16 or bfloat16, the products' type) [n_out, ceil(n_in /
+    group)] for ecasq_matvec."""
+    _half_tensor(scales, "scales")
+    if symbols.dim() != 2 or symbols.dtype != torch.uint8 or symbols.device != scales.device:
+        raise TypeError("symbols must be a uint8 tensor [n_out, n_in] on the scales' device")
+    n_out, n_in = symbols.shape
+    group = int(group)
+    size = lib().ecasq_weights_size(n_out, n_in, group)
+    if size == 0:
+        raise ValueError("sizes or group out of range")
+    if tuple(scales.shape) != (n_out, -(-n_in // group)):
+        raise ValueError("scales must be [n_out, ceil(n_in / group)]")
+    with _on(scales.device, stream) as st:
+        cb = codebook.to(device=scales.device, dtype=torch.float64).contiguous().reshape(-1)
+        packed = torch.empty(size, dtype=torch.uint8, device=scales.device)
+        symbols, scales = symbols.contiguous(), scales.contiguous()
+        _raise(lib().ecasq_weights_pack(symbols.data_ptr(), cb.data_ptr(), cb.numel(),
+                                        scales.data_ptr(), _HALF[scales.dtype], n_out, n_in, group,
+                                        st, packed.data_ptr(), size))
+    return ecasq_weights(packed, scales.dtype, n_out, n_in, group)
+
+
+def ecasq_matvec(w, x, out=None, stream=None):
+    """y = W x for every row of x [..., n_in]; returns y [..., n_out]."""
+    packed = w.packed
+    if not isinstance(x, torch.Tensor) or x.dtype != w.dtype or x.device != packed.device:
+        raise TypeError(f"x must be a {w.dtype} tensor on {packed.device}")
+    if x.dim() == 0 or x.shape[-1] != w.n_in:
+        raise ValueError(f"x must end in {w.n_in} entries")
+    shape = x.shape[:-1] + (w.n_out,)
+    with _on(packed.device, stream) as st:
+        if x.dim() == 2 and x.stride(1) == 1 and x.stride(0) >= w.n_in:
+            m, step = x.shape[0], x.stride(0)
+        else:
+            x = x.reshape(-1, w.n_in).contiguous()
+            m, step = x.shape[0], w.n_in
+        if out is None:
+            out = torch.empty(shape, dtype=w.dtype, device=packed.device)
+        else:
+            _tensor(out, "out", w.dtype, packed.device, shape)
+        if m:
+            _raise(lib().ecasq_matvec(packed.data_ptr(), _HALF[w.dtype], w.n_out, w.n_in, w.group,
+                                      x.data_ptr(), m, step, st, out.data_ptr()))
+    return out
+
+
+class ecasq_kv_cache:
+    """A paged key/value cache over the caller's tensors, which it keeps and which
+    are updated in place (another tensor cannot take an old one's name):
+    k, v [n_pages, heads, page_size, head_dim] of float16 or bfloat16, or uint8
+    [..., head_dim / 2] with k_books, v_books [n_pages, heads, page_size, 16];
+    table int32 [batch, max_pages]; lens int32 [batch]; mass float32 and pos int32
+    [batch, heads, max_pages * page_size], each where it is needed."""
+
+    def __init__(self, k, v, table, lens, k_books=None, v_books=None, mass=None, pos=None):
+        if not isinstance(k, torch.Tensor) or not k.is_cuda or k.dim() != 4:
+            raise TypeError("k must be a CUDA (HIP) tensor [n_pages, heads, page_size, entries]")
+        self.coded = k.dtype == torch.uint8
+        if self.coded and (k_books is None or v_books is None):
+            raise ValueError("a cache of symbols needs k_books and v_books")
+        if not self.coded and (k_books is not None or v_books is not None):
+            raise ValueError("a cache of rows has no codebooks")
+        self.dtype = _half_tensor(k_books if self.coded else k, "k").dtype
+        dev = self.device = k.device
+        self.n_pages, self.heads, self.page_size, last = k.shape
+        self.head_dim = 2 * last if self.coded else last
+        if not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise TypeError("table must be an int32 tensor [batch, max_pages]")
+        self.batch, self.max_pages = table.shape
+        self.slots = self.max_pages * self.page_size
+        self.k, self.v = _tensor(k, "k", k.dtype, dev), _tensor(v, "v", k.dtype, dev, k.shape)
+        self.k_books, self.v_books, self.mass, self.pos = k_books, v_books, mass, pos
+        self.table = _tensor(table, "table", torch.int32, dev)
+        self.lens = _tensor(lens, "lens", torch.int32, dev, (self.batch,))
+        if self.coded:
+            for name, x in (("k_books", k_books), ("v_books", v_books)):
+                _tensor(x, name, self.dtype, dev, k.shape[:3] + (16,))
+        self._slots_shape = (self.batch, self.heads, self.slots)
+        if mass is not None:
+            _tensor(mass, "mass", torch.float32, dev, self._slots_shape)
+        if pos is not None:
+            _tensor(pos, "pos", torch.int32, dev, self._slots_shape)
+        self._c = _kv_struct(_HALF[self.dtype], int(self.coded), self.heads, self.head_dim,
+                             self.page_size, self.batch, self.max_pages, self.n_pages,
+                             *[x.data_ptr() if x is not None else None for x in
+                               (k, v, k_books, v_books, table, lens, mass, pos)])
+        self._sizes = {}
+
+    def __setattr__(self, name, value):
+        if "_sizes" in self.__dict__ and self.__dict__.get(name) is not value:
+            raise AttributeError(f"{name} is set once: update the cache's tensors in place")
+        self.__dict__[name] = value
+
+    def _workspace(self, name, *args):
+        """A workspace of the size that the library's function `name` says."""
+        key = (name,) + args
+        size = self._sizes.get(key)
+        if size is None:
+            size = getattr(lib(), name)(ctypes.byref(self._c), *args)
+            if size == 0:
+                raise EcasqError(ECASQ_EINVAL)
+            self._sizes[key] = size
+        return torch.empty(size, dtype=torch.uint8, device=self.device), size
+
+
+def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=None,
+                   v_codebooks=None, v_counts=None, seed=0, k_hat=None, v_hat=None, stream=None):
+    """Writes new tokens' rows k, v [rows, heads, head_dim] into the cache, rows
+    starts[b] .. starts[b+1]-1 (int32, device) at the end of sequence b, whose lens
+    already counts them.  A cache of symbols takes the rows' codebooks and counts
+    as ecasq_solve_batched returns them for k.reshape(rows * heads, head_dim), and
+    gives back the rounded rows in k_hat, v_hat where they are given."""
+    dev, inner = kv.device, kv.heads * kv.head_dim
+    for name, x in (("k", k), ("v", v)):
+        if not isinstance(x, torch.Tensor) or x.dtype != kv.dtype or x.device != dev:
+            raise TypeError(f"{name} must be a {kv.dtype} tensor on {dev}")
+        if x.dim() != 3 or x.shape[1:] != (kv.heads, kv.head_dim) or x.shape[0] != k.shape[0]:
+            raise ValueError(f"{name} must be [rows, {kv.heads}, {kv.head_dim}]")
+    rows = k.shape[0]
+    _tensor(starts, "starts", torch.int32, dev, (kv.batch + 1,))
+    if positions is not None:
+        _tensor(positions, "positions", torch.int32, dev, (rows,))
+    s, books = 0, [None] * 4
+    if kv.coded:
+        if k_codebooks is None or v_codebooks is None or k_counts is None or v_counts is None:
+            raise ValueError("a cache of symbols needs the rows' codebooks and counts")
+        s = k_codebooks.shape[-1]
+        for name, x in (("k_codebooks", k_codebooks), ("v_codebooks", v_codebooks)):
+            _tensor(x, name, torch.float64, dev, (rows * kv.heads, s))
+        for name, x in (("k_counts", k_counts), ("v_counts", v_counts)):
+            _tensor(x, name, torch.int32, dev, (rows * kv.heads,))
+        books = [x.data_ptr() for x in (k_codebooks, k_counts, v_codebooks, v_counts)]
+        for name, x in (("k_hat", k_hat), ("v_hat", v_hat)):
+            if x is not None:
+                _tensor(x, name, kv.dtype, dev, (rows, kv.heads, kv.head_dim))
+    elif k_codebooks is not None or v_codebooks is not None:
+        raise ValueError("a cache of rows takes no codebooks")
+    if rows == 0:
+        return
+    with _on(dev, stream) as st:
+        k, ks = _rows_apart(k, inner)
+        v, vs = _rows_apart(v, inner)
+        _raise(lib().ecasq_kv_write(ctypes.byref(kv._c), k.data_ptr(), ks, v.data_ptr(), vs, rows,
+                                    starts.data_ptr(),
+                                    positions.data_ptr() if positions is not None else None, st,
+                                    *books, s, int(seed) & (2 ** 64 - 1),
+                                    k_hat.data_ptr() if k_hat is not None else None,
+                                    v_hat.data_ptr() if v_hat is not None else None))
+
+
+def ecasq_kv_attention(kv, q, scale=None, mass_out=None, out=None, stream=None):
+    """Attention of one token per sequence, q [batch, q_heads, head_dim], over the
+    cache; scale: 1 / sqrt(head_dim) if None.  With mass_out (float32, as
+    kv.mass, which it may be) the weights of the slots are added to kv.mass there.
+    Returns out [batch, q_heads, head_dim]."""
+    if not isinstance(q, torch.Tensor) or q.dtype != kv.dtype or q.device != kv.device:
+        raise TypeError(f"q must be a {kv.dtype} tensor on {kv.device}")
+    if q.dim() != 3 or q.shape[0] != kv.batch or q.shape[2] != kv.head_dim:
+        raise ValueError(f"q must be [{kv.batch}, q_heads, {kv.head_dim}]")
+    q_heads = q.shape[1]
+    if mass_out is not None:
+        _tensor(mass_out, "mass_out", torch.float32, kv.device, kv._slots_shape)
+    with _on(kv.device, stream) as st:
+        q, step = _rows_apart(q, q_heads * kv.head_dim)
+        if out is None:
+            out = torch.empty((kv.batch, q_heads, kv.head_dim), dtype=kv.dtype, device=kv.device)
+        else:
+            _tensor(out, "out", kv.dtype, kv.device, (kv.batch, q_heads, kv.head_dim))
+        ws, size = kv._workspace("ecasq_kv_attention_workspace", q_heads,
+                                 int(mass_out is not None))
+        _raise(lib().ecasq_kv_attention(ctypes.byref(kv._c), q.data_ptr(), step, q_heads,
+                                        kv.head_dim ** -0.5 if scale is None else float(scale),
+                                        mass_out.data_ptr() if mass_out is not None else None, st,
+                                        out.data_ptr(), ws.data_ptr(), size))
+    return out
+
+
+def ecasq_kv_evict(kv, keep, recent=0, mass_out=None, pos_out=None, lens_out=None, stream=None):
+    """Every head of a sequence with more than `keep` slots gives up all but
+    those of the `recent` newest positions and the largest mass; the kept rows
+    are moved below slot `keep`.  kv.mass, kv.pos and kv.lens are updated, or the
+    tensors given for them in their place."""
+    if kv.mass is None or kv.pos is None:
+        raise ValueError("the cache needs mass and pos")
+    mass_out = kv.mass if mass_out is None else \
+        _tensor(mass_out, "mass_out", torch.float32, kv.device, kv._slots_shape)
+    pos_out = kv.pos if pos_out is None else \
+        _tensor(pos_out, "pos_out", torch.int32, kv.device, kv._slots_shape)
+    lens_out = kv.lens if lens_out is None else \
+        _tensor(lens_out, "lens_out", torch.int32, kv.device, (kv.batch,))
+    keep, recent = int(keep), int(recent)
+    with _on(kv.device, stream) as st:
+        ws, size = kv._workspace("ecasq_kv_evict_workspace", keep)
+        _raise(lib().ecasq_kv_evict(ctypes.byref(kv._c), keep, recent, mass_out.data_ptr(),
+                                    pos_out.data_ptr(), lens_out.data_ptr(), st, ws.data_ptr(),
+                                    size))
 
 
 def infos_to_dicts(infos):
