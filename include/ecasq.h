@@ -417,8 +417,8 @@ ecasq_status ecasq_matvec(const void *packed, ecasq_dtype dt, int64_t n_out, int
  *     v_books [n_pages][heads][page_size][16] of dt, each row's own codebook
  *     (ecasq_solve_batched): 4 + 256 / head_dim bits an entry.
  * dt is ECASQ_F16 or ECASQ_BF16; head_dim 64, 128 or 256; page_size a multiple
- * of 16, 16 to 65536; 1 <= heads <= 1024; 1 <= batch <= 65535; k, v and the
- * books are 16-byte aligned.  lens[b] is the number of slots of sequence b in
+ * of 16, 16 to 65536, and max_pages page_size at most 2^30; 1 <= heads <= 1024;
+ * 1 <= batch <= 65535; k, v and the books are 16-byte aligned.  lens[b] is the number of slots of sequence b in
  * use; a number below 0 counts as 0, one above max_pages page_size as that.  The
  * slots of a table entry outside [0, n_pages) hold nothing: they are not read,
  * not written, and get no weight.  A page with slots that a call writes must
@@ -484,7 +484,7 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  *   scale q[b][h] . K[b][g][t],  g = h heads / q_heads;
  * q: device, batch rows of q_heads x head_dim entries of dt, q_stride >= q_heads
  * head_dim entries apart, of their type's alignment; q_heads a multiple of heads,
- * at most 64 heads; out: device, batch x q_heads x head_dim of dt, 16-byte
+ * at most 64 heads, and batch q_heads at most 2^28; out: device, batch x q_heads x head_dim of dt, 16-byte
  * aligned.  Scores, weights and sums are fp32; out is rounded once.  A sequence
  * with no slots to read, or whose scores are all -inf, gives zeros.  A NaN or
  * infinity in a row that is read reaches the result; what lies in slots past

@@ -28,7 +28,7 @@ bool kv_sizes_ok(const ecasq_kv_cache* c) {
            c->heads <= 1024 && (c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256) &&
            c->page_size >= 16 && c->page_size <= 65536 && c->page_size % 16 == 0 &&
            c->batch >= 1 && c->batch <= 65535 && c->max_pages >= 1 && c->n_pages >= 1 &&
-           kv_slots(*c) < ((int64_t)1 << 31);
+           kv_slots(*c) <= ((int64_t)1 << 30);
 }
 
 bool kv_ok(const ecasq_kv_cache* c) {
@@ -39,7 +39,8 @@ bool kv_ok(const ecasq_kv_cache* c) {
 }
 
 bool heads_ok(const ecasq_kv_cache* c, int32_t q_heads) {
-    return q_heads >= c->heads && q_heads % c->heads == 0 && q_heads / c->heads <= 64;
+    return q_heads >= c->heads && q_heads % c->heads == 0 && q_heads / c->heads <= 64 &&
+           (int64_t)c->batch * q_heads <= ((int64_t)1 << 28);
 }
 
 ecasq_status status(hipError_t e) { return e == hipSuccess ? ECASQ_OK : ECASQ_EHIP; }
