@@ -25,6 +25,9 @@ typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+#ifndef WPE
+#define WPE 3
+#endif
 constexpr int kWaves = 4, kAT = 64 * kWaves;
 constexpr float kLazy = 8.0f;  // log2 of what a weight may pass 1 by
 template <int DT>
@@ -132,7 +135,7 @@ struct Tile {
 constexpr int kBookBytes = 1280;
 
 template <int DT, bool CODED, int D>
-__global__ __launch_bounds__(kAT) void k_attend(ecasq_kv_cache c, Plan p,
+__global__ __launch_bounds__(kAT, D == 256 ? 2 : WPE) void k_attend(ecasq_kv_cache c, Plan p,
                                                 const uint16_t* __restrict__ q, int64_t q_stride,
                                                 float scale, uint16_t* __restrict__ out,
                                                 float* __restrict__ scores,
@@ -197,6 +200,11 @@ __global__ __launch_bounds__(kAT) void k_attend(ecasq_kv_cache c, Plan p,
         return r;
     };
 
+    // where a lane's part of a tile's keys and values begins, in bytes
+    constexpr uint32_t kRow = CODED ? D / 2 : 2 * D;
+    const uint32_t k_at = n16 * kRow + g * (CODED ? D / 8 : 16);
+    const uint32_t v_at = 4 * g * kRow + n16 * (kRow / 16);
+
     f32x4 acc[E];
 #pragma unroll
     for (int i = 0; i < E; i++) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -214,18 +222,18 @@ __global__ __launch_bounds__(kAT) void k_attend(ecasq_kv_cache c, Plan p,
             Words<8> kb[2];
 #pragma unroll
             for (int t = 0; t < 2; t++) {
-                const int64_t row = tile[t].row + n16;
-                kc[t] = load_words<D / 32>(static_cast<const uint8_t*>(c.k) + row * (D / 2) +
-                                           g * (D / 8));
-                kb[t] = load_words<8>(static_cast<const uint8_t*>(c.k_books) + row * 32);
+                kc[t] = load_words<D / 32>(static_cast<const uint8_t*>(c.k) +
+                                           tile[t].row * (D / 2) + k_at);
+                kb[t] = load_words<8>(static_cast<const uint8_t*>(c.k_books) + tile[t].row * 32 +
+                                      n16 * 32u);
             }
+            const int64_t vb_row = lane < 32 ? tile[0].row : tile[1].row;
             const Words<4> vb = load_words<4>(static_cast<const uint8_t*>(c.v_books) +
-                                              (tile[lane / 32].row + lane / 2 % 16) * 32 +
-                                              lane % 2 * 16);
+                                              vb_row * 32 + lane % 32 * 16);
 #pragma unroll
             for (int k = 0; k < 8; k++) {
-                const uint8_t* at = static_cast<const uint8_t*>(c.v) +
-                                    (tile[k / 4].row + 4 * g + k % 4) * (D / 2) + n16 * (E / 2);
+                const uint8_t* at = static_cast<const uint8_t*>(c.v) + tile[k / 4].row * (D / 2) +
+                                    v_at + k % 4 * (D / 2);
                 if constexpr (E == 4)
                     v[k].w[0] = *reinterpret_cast<const uint16_t*>(at);
                 else
@@ -233,7 +241,7 @@ __global__ __launch_bounds__(kAT) void k_attend(ecasq_kv_cache c, Plan p,
             }
             {
                 const int slot = lane / 2 % 16;
-                const bool live = slot < tile[lane / 32].live;
+                const bool live = slot < (lane < 32 ? tile[0].live : tile[1].live);
                 uint8_t* to = book + slot / 4 * 288 + (slot % 4 + lane / 32 * 4) * 32 +
                               lane % 2 * 16;
                 Words<4> w;
@@ -255,12 +263,11 @@ __global__ __launch_bounds__(kAT) void k_attend(ecasq_kv_cache c, Plan p,
 #pragma unroll
                 for (int j = 0; j < J; j++)
                     kv[t][j] = *reinterpret_cast<const u32x4*>(
-                        static_cast<const uint16_t*>(c.k) + (tile[t].row + n16) * D + 32 * j +
-                        8 * g);
+                        static_cast<const uint8_t*>(c.k) + tile[t].row * (2 * D) + k_at + 64 * j);
 #pragma unroll
             for (int k = 0; k < 8; k++)
-                v[k] = load_words<E / 2>(static_cast<const uint16_t*>(c.v) +
-                                         (tile[k / 4].row + 4 * g + k % 4) * D + n16 * E);
+                v[k] = load_words<E / 2>(static_cast<const uint8_t*>(c.v) +
+                                         tile[k / 4].row * (2 * D) + v_at + k % 4 * (2 * D));
 #pragma unroll
             for (int t = 0; t < 2; t++) {
                 s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -291,16 +298,20 @@ __global__ __launch_bounds__(kAT) void k_attend(ecasq_kv_cache c, Plan p,
                                               4 * g) = w;
                 }
         }
+        float down = 1.0f;
         if (__any(top > m + kLazy)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float M = fmaxf(m, top), down = down_to(m, M);
+            const float M = fmaxf(m, top);
+            down = down_to(m, M);
             m = M;
             ref = M == -INFINITY ? 0.0f : M - kLift<DT>;
-            l *= down;
-#pragma unroll
-            for (int i = 0; i < E; i++) acc[i] *= down;
         }
+        // by 1 where nothing moved: 32 products cost less than the copies of O' that the
+        // compiler makes where a branch may change it
+        l *= down;
+#pragma unroll
+        for (int i = 0; i < E; i++) acc[i] *= down;
         u32x4 hi, rest;
         float w[8];
 #pragma unroll
@@ -415,11 +426,44 @@ __global__ __launch_bounds__(kAT) void k_attend(ecasq_kv_cache c, Plan p,
 // key/value head at a time: the sum over the group's heads in order.
 constexpr int kJT = 256;
 
+// Maximum and sum of a head's chunks, by one wavefront; the same for every lane.
 __device__ __forceinline__ float2 joined(const float2* __restrict__ ml, int32_t used) {
+    const int lane = threadIdx.x % 64;
     float m = -INFINITY, l = 0.0f;
-    for (int32_t k = 0; k < used; k++) m = fmaxf(m, ml[k].x);
-    for (int32_t k = 0; k < used; k++) l += ml[k].y * down_to(ml[k].x, m);
+    for (int32_t k = lane; k < used; k += 64) m = fmaxf(m, ml[k].x);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+    for (int32_t k = lane; k < used; k += 64) l += ml[k].y * down_to(ml[k].x, m);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
     return make_float2(m, l);
+}
+
+template <int DT, int D>
+__device__ __forceinline__ void join_row(const Plan& p, int64_t row, int32_t used,
+                                         const float2* __restrict__ ml,
+                                         const float* __restrict__ part,
+                                         uint16_t* __restrict__ out) {
+    // a chunk's entries by D / 4 threads, kSide chunks side by side
+    constexpr int kSide = kJT / (D / 4);
+    __shared__ f32x4 sums[kJT];
+    const int side = threadIdx.x / (D / 4), e = threadIdx.x % (D / 4);
+    const float2* at = ml + row * p.chunks;
+    const float2 all = joined(at, used);
+    const auto* from = reinterpret_cast<const f32x4*>(part + row * p.chunks * D) + e;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int32_t k = side; k < used; k += kSide)
+        o += from[(int64_t)k * (D / 4)] * down_to(at[k].x, all.x);
+    sums[threadIdx.x] = o;
+    __syncthreads();
+    if (side != 0) return;
+#pragma unroll
+    for (int k = 1; k < kSide; k++) o += sums[k * (D / 4) + e];
+    const float by = all.y == 0.0f ? 0.0f : 1.0f / all.y;
+    const uint32_t w[2] = {to16<DT>(o[0] * by) | (uint32_t)to16<DT>(o[1] * by) << 16,
+                           to16<DT>(o[2] * by) | (uint32_t)to16<DT>(o[3] * by) << 16};
+    __builtin_memcpy(__builtin_assume_aligned(out + row * D + 4 * e, 8), w, 8);
 }
 
 template <int DT>
@@ -432,14 +476,13 @@ __global__ __launch_bounds__(kJT) void k_join(ecasq_kv_cache c, Plan p, int32_t 
         const int64_t row = blockIdx.x;
         const int32_t b = (int32_t)(row / p.q_heads);
         const int32_t n = (int32_t)kv_len(c, b), used = (n + p.chunk - 1) / p.chunk;
-        const int e = threadIdx.x;
-        if (used <= 1 || e >= c.head_dim) return;
-        const float2* at = ml + row * p.chunks;
-        const float2 all = joined(at, used);
-        float o = 0.0f;
-        for (int32_t k = 0; k < used; k++)
-            o += part[(row * p.chunks + k) * c.head_dim + e] * down_to(at[k].x, all.x);
-        out[row * c.head_dim + e] = to16<DT>(all.y == 0.0f ? 0.0f : o / all.y);
+        if (used <= 1) return;
+        if (c.head_dim == 64)
+            join_row<DT, 64>(p, row, used, ml, part, out);
+        else if (c.head_dim == 128)
+            join_row<DT, 128>(p, row, used, ml, part, out);
+        else
+            join_row<DT, 256>(p, row, used, ml, part, out);
         return;
     }
     __shared__ float2 each[64];
@@ -451,10 +494,11 @@ __global__ __launch_bounds__(kJT) void k_join(ecasq_kv_cache c, Plan p, int32_t 
     const int32_t first = (int32_t)(id % spans) * kJT;
     if (first >= n) return;
     const int32_t used = (n + p.chunk - 1) / p.chunk;
-    if ((int)threadIdx.x < p.group) {
-        const float2 v = joined(ml + (kvh * p.group + threadIdx.x) * p.chunks, used);
-        each[threadIdx.x] = make_float2(v.x == -INFINITY ? 0.0f : v.x - kLift<DT>,
-                                        v.y == 0.0f ? 0.0f : 1.0f / v.y);
+    for (int32_t h = threadIdx.x / 64; h < p.group; h += kJT / 64) {
+        const float2 v = joined(ml + (kvh * p.group + h) * p.chunks, used);
+        if (threadIdx.x % 64 == 0)
+            each[h] = make_float2(v.x == -INFINITY ? 0.0f : v.x - kLift<DT>,
+                                  v.y == 0.0f ? 0.0f : 1.0f / v.y);
     }
     __syncthreads();
     const int32_t i = first + (int32_t)threadIdx.x;
@@ -471,7 +515,10 @@ size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 // Workgroups of four wavefronts: about kGroups of them where every sequence is as
 // long as the table allows, 128 slots each at least.
-constexpr int64_t kGroups = 1024;
+#ifndef GROUPS
+#define GROUPS 1024
+#endif
+constexpr int64_t kGroups = GROUPS;
 
 Plan plan(const ecasq_kv_cache& c, int32_t q_heads) {
     Plan p;
