@@ -25,9 +25,6 @@ typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-#ifndef WPE
-#define WPE 3
-#endif
 constexpr int kWaves = 4, kAT = 64 * kWaves;
 constexpr float kLazy = 8.0f;  // log2 of what a weight may pass 1 by
 template <int DT>
@@ -135,7 +132,7 @@ struct Tile {
 constexpr int kBookBytes = 1280;
 
 template <int DT, bool CODED, int D>
-__global__ __launch_bounds__(kAT, D == 256 ? 2 : WPE) void k_attend(ecasq_kv_cache c, Plan p,
+__global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache c, Plan p,
                                                 const uint16_t* __restrict__ q, int64_t q_stride,
                                                 float scale, uint16_t* __restrict__ out,
                                                 float* __restrict__ scores,
@@ -148,13 +145,17 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : WPE) void k_attend(ecasq_kv_cac
 
     const int lane = threadIdx.x % 64, n16 = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    // workgroups: chunk, then head tile, head and sequence
+    // workgroups: head, then sequence, head tile and chunk.  Workgroups go to the eight
+    // dies in turn; with the chunks first, the first chunks, which every sequence has,
+    // came to lie on one die and the last ones on another (16 ragged sequences: 3 of 53 us).
+    // The tiles of a head meet on one die where
+    // the heads of all sequences are a multiple of eight.
     int32_t id = blockIdx.x;
-    const int32_t ch = id % p.chunks;
-    id /= p.chunks;
-    const int32_t ht = id % p.tiles;
-    id /= p.tiles;
-    const int32_t head = id % c.heads, b = id / c.heads;
+    const int32_t head = id % c.heads;
+    id /= c.heads;
+    const int32_t b = id % c.batch;
+    id /= c.batch;
+    const int32_t ht = id % p.tiles, ch = id / p.tiles;
     const int32_t n = (int32_t)kv_len(c, b);
     const int32_t lo = ch * p.chunk;
     if (lo >= n && ch > 0) return;
@@ -422,9 +423,9 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : WPE) void k_attend(ecasq_kv_cac
 }
 
 // Joins the chunks of every sequence that has more than one, a workgroup per query
-// head; the workgroups after those give the slots their weights, 256 slots of a
+// head; the workgroups after those give the slots their weights, 1024 slots of a
 // key/value head at a time: the sum over the group's heads in order.
-constexpr int kJT = 256;
+constexpr int kJT = 256, kSpan = 4 * kJT;
 
 // Maximum and sum of a head's chunks, by one wavefront; the same for every lane.
 __device__ __forceinline__ float2 joined(const float2* __restrict__ ml, int32_t used) {
@@ -487,11 +488,11 @@ __global__ __launch_bounds__(kJT) void k_join(ecasq_kv_cache c, Plan p, int32_t 
     }
     __shared__ float2 each[64];
     const int64_t slots = kv_slots(c);
-    const int32_t spans = (int32_t)((slots + kJT - 1) / kJT);
+    const int32_t spans = (int32_t)((slots + kSpan - 1) / kSpan);
     const int64_t id = (int64_t)blockIdx.x - join_groups;
     const int64_t kvh = id / spans;
     const int32_t b = (int32_t)(kvh / c.heads), n = (int32_t)kv_len(c, b);
-    const int32_t first = (int32_t)(id % spans) * kJT;
+    const int32_t first = (int32_t)(id % spans) * kSpan;
     if (first >= n) return;
     const int32_t used = (n + p.chunk - 1) / p.chunk;
     for (int32_t h = threadIdx.x / 64; h < p.group; h += kJT / 64) {
@@ -501,24 +502,31 @@ __global__ __launch_bounds__(kJT) void k_join(ecasq_kv_cache c, Plan p, int32_t 
                                   v.y == 0.0f ? 0.0f : 1.0f / v.y);
     }
     __syncthreads();
-    const int32_t i = first + (int32_t)threadIdx.x;
+    const int32_t i = first + 4 * (int32_t)threadIdx.x;
     if (i >= n) return;
-    float w = 0.0f;
-    for (int32_t h = 0; h < p.group; h++)
-        w += __builtin_amdgcn_exp2f(scores[(kvh * p.group + h) * slots + i] - each[h].x) *
-             each[h].y;
+    // four slots: all within the row of scores, whose length is a multiple of 16
+    f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t h = 0; h < p.group; h++) {
+        const f32x4 z = *reinterpret_cast<const f32x4*>(scores + (kvh * p.group + h) * slots + i);
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+            w[k] += __builtin_amdgcn_exp2f(z[k] - each[h].x) * each[h].y;
+    }
     const int64_t at = kvh * slots + i;
-    mass_out[at] = (c.mass ? c.mass[at] : 0.0f) + w;
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+        if (i + k < n) mass_out[at + k] = (c.mass ? c.mass[at + k] : 0.0f) + w[k];
 }
 
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-// Workgroups of four wavefronts: about kGroups of them where every sequence is as
-// long as the table allows, 128 slots each at least.
-#ifndef GROUPS
-#define GROUPS 1024
-#endif
-constexpr int64_t kGroups = GROUPS;
+// Workgroups of four wavefronts where every sequence is as long as the table allows: as
+// many as are resident at once for a single sequence; more for several, because
+// they seldom are of one length (131071 coded slots alone: 54 us with 1024, 60 with
+// 1792; 16 sequences of 0 to 8191: 49 and 39 us; 64 of 3500 to 4500 in 16 bits: 190 and
+// 193 us).  A chunk has 256 slots at least: two rounds of a workgroup take less than
+// the launch that joins two chunks (4 sequences of up to 200: 6.9 us, 8.5 with 128).
+constexpr int64_t kGroupsOne = 1024, kGroupsMany = 1792, kChunkLeast = 256;
 
 Plan plan(const ecasq_kv_cache& c, int32_t q_heads) {
     Plan p;
@@ -526,9 +534,10 @@ Plan plan(const ecasq_kv_cache& c, int32_t q_heads) {
     p.group = q_heads / c.heads;
     p.tiles = (p.group + 15) / 16;
     const int64_t rows = (int64_t)c.batch * c.heads * p.tiles, slots = kv_slots(c);
-    int64_t chunk = (rows * slots + kGroups - 1) / kGroups;
+    const int64_t groups = c.batch > 1 ? kGroupsMany : kGroupsOne;
+    int64_t chunk = (rows * slots + groups - 1) / groups;
     chunk = (chunk + 127) / 128 * 128;
-    if (chunk < 128) chunk = 128;
+    if (chunk < kChunkLeast) chunk = kChunkLeast;
     if (chunk > slots) chunk = slots;
     p.chunk = (int32_t)chunk;
     p.chunks = (int32_t)((slots + chunk - 1) / chunk);
@@ -592,7 +601,7 @@ hipError_t launch_kv_attention(const ecasq_kv_cache& c, const void* q, int64_t q
     if (e != hipSuccess || (p.chunks == 1 && !mass_out)) return e;
     const int32_t join = p.chunks > 1 ? c.batch * q_heads : 0;
     const int64_t weigh =
-        mass_out ? (int64_t)c.batch * c.heads * ((kv_slots(c) + kJT - 1) / kJT) : 0;
+        mass_out ? (int64_t)c.batch * c.heads * ((kv_slots(c) + kSpan - 1) / kSpan) : 0;
     if (c.dt == ECASQ_F16)
         k_join<1><<<(unsigned)(join + weigh), kJT, 0, st>>>(c, p, join, scores, ml, part, o,
                                                             mass_out);

@@ -457,24 +457,28 @@ class _on:
     def __init__(self, device, stream):
         if stream is not None and stream.device != device:
             raise ValueError(f"the stream must be on {device}")
-        self.was = None
-        if torch.cuda.current_device() != device.index:
-            self.was = torch.cuda.device(device)
-            self.was.__enter__()
-        self.stream = None
-        if stream is not None:
-            self.stream = torch.cuda.stream(stream)
-            self.stream.__enter__()
-        self.ptr = torch.cuda.current_stream().cuda_stream
+        self.device, self.stream = torch.cuda.device(device), stream
 
     def __enter__(self):
-        return self.ptr
+        self.device.__enter__()
+        if self.stream is not None:
+            self.stream = torch.cuda.stream(self.stream)
+            self.stream.__enter__()
 
     def __exit__(self, *exc):
         if self.stream is not None:
             self.stream.__exit__(*exc)
-        if self.was is not None:
-            self.was.__exit__(*exc)
+        self.device.__exit__(*exc)
+
+
+def _run(f, device, stream, *args):
+    """f(stream, *args) with the device and the stream as torch's current ones,
+    which most calls find that way (the contexts cost as much as a small kernel)."""
+    index = device.index
+    if stream is None and torch._C._cuda_getDevice() == index:
+        return f(torch._C._cuda_getCurrentRawStream(index), *args)
+    with _on(device, stream):
+        return f(torch._C._cuda_getCurrentRawStream(index), *args)
 
 
 def _tensor(x, name, dtype, device, shape=None):
@@ -495,25 +499,26 @@ def _half_tensor(x, name):
 
 
 def _rows_apart(x, inner):
-    """x as rows of `inner` entries and the entries between their starts; copied
-    where they do not lie that way."""
-    x = x.reshape(-1, inner) if x.is_contiguous() else x
-    flat, want = x.shape[0] if x.dim() else 1, 1
+    """x [rows, ...] whose rows of `inner` entries are contiguous, and the entries
+    between their starts; copied where they do not lie that way."""
+    if x.is_contiguous():
+        return x, inner
+    want = 1
     for size, step in zip(reversed(x.shape[1:]), reversed(x.stride()[1:])):
         if size != 1 and step != want:
             return x.contiguous(), inner
         want *= size
-    step = x.stride(0) if flat > 1 else inner
+    step = x.stride(0) if x.shape[0] > 1 else inner
     return (x, step) if step >= inner else (x.contiguous(), inner)
 
 
 class ecasq_weights:
     """A packed 4-bit weight matrix (ecasq_weights_pack)."""
 
-    __slots__ = ("packed", "dtype", "n_out", "n_in", "group")
+    __slots__ = ("packed", "dtype", "device", "n_out", "n_in", "group")
 
     def __init__(self, packed, dtype, n_out, n_in, group):
-        self.packed, self.dtype = packed, dtype
+        self.packed, self.dtype, self.device = packed, dtype, packed.device
         self.n_out, self.n_in, self.group = n_out, n_in, group
 
 
@@ -522,7 +527,8 @@ def ecasq_weights_pack(symbols, codebook, scales, group, stream=None):
     and scales (float16 or bfloat16, the products' type) [n_out, ceil(n_in /
     group)] for ecasq_matvec."""
     _half_tensor(scales, "scales")
-    if symbols.dim() != 2 or symbols.dtype != torch.uint8 or symbols.device != scales.device:
+    if not isinstance(symbols, torch.Tensor) or symbols.dim() != 2 or \
+            symbols.dtype != torch.uint8 or symbols.device != scales.device:
         raise TypeError("symbols must be a uint8 tensor [n_out, n_in] on the scales' device")
     n_out, n_in = symbols.shape
     group = int(group)
@@ -531,37 +537,43 @@ def ecasq_weights_pack(symbols, codebook, scales, group, stream=None):
         raise ValueError("sizes or group out of range")
     if tuple(scales.shape) != (n_out, -(-n_in // group)):
         raise ValueError("scales must be [n_out, ceil(n_in / group)]")
-    with _on(scales.device, stream) as st:
-        cb = codebook.to(device=scales.device, dtype=torch.float64).contiguous().reshape(-1)
-        packed = torch.empty(size, dtype=torch.uint8, device=scales.device)
-        symbols, scales = symbols.contiguous(), scales.contiguous()
-        _raise(lib().ecasq_weights_pack(symbols.data_ptr(), cb.data_ptr(), cb.numel(),
-                                        scales.data_ptr(), _HALF[scales.dtype], n_out, n_in, group,
-                                        st, packed.data_ptr(), size))
+    return _run(_pack, scales.device, stream, symbols, codebook, scales, group, size)
+
+
+def _pack(st, symbols, codebook, scales, group, size):
+    n_out, n_in = symbols.shape
+    cb = codebook.to(device=scales.device, dtype=torch.float64).contiguous().reshape(-1)
+    packed = torch.empty(size, dtype=torch.uint8, device=scales.device)
+    symbols, scales = symbols.contiguous(), scales.contiguous()
+    _raise(lib().ecasq_weights_pack(symbols.data_ptr(), cb.data_ptr(), cb.numel(),
+                                    scales.data_ptr(), _HALF[scales.dtype], n_out, n_in, group,
+                                    st, packed.data_ptr(), size))
     return ecasq_weights(packed, scales.dtype, n_out, n_in, group)
 
 
 def ecasq_matvec(w, x, out=None, stream=None):
     """y = W x for every row of x [..., n_in]; returns y [..., n_out]."""
-    packed = w.packed
-    if not isinstance(x, torch.Tensor) or x.dtype != w.dtype or x.device != packed.device:
-        raise TypeError(f"x must be a {w.dtype} tensor on {packed.device}")
+    if not isinstance(x, torch.Tensor) or x.dtype != w.dtype or x.device != w.device:
+        raise TypeError(f"x must be a {w.dtype} tensor on {w.device}")
     if x.dim() == 0 or x.shape[-1] != w.n_in:
         raise ValueError(f"x must end in {w.n_in} entries")
-    shape = x.shape[:-1] + (w.n_out,)
-    with _on(packed.device, stream) as st:
-        if x.dim() == 2 and x.stride(1) == 1 and x.stride(0) >= w.n_in:
-            m, step = x.shape[0], x.stride(0)
-        else:
-            x = x.reshape(-1, w.n_in).contiguous()
-            m, step = x.shape[0], w.n_in
-        if out is None:
-            out = torch.empty(shape, dtype=w.dtype, device=packed.device)
-        else:
-            _tensor(out, "out", w.dtype, packed.device, shape)
-        if m:
-            _raise(lib().ecasq_matvec(packed.data_ptr(), _HALF[w.dtype], w.n_out, w.n_in, w.group,
-                                      x.data_ptr(), m, step, st, out.data_ptr()))
+    if out is not None:
+        _tensor(out, "out", w.dtype, w.device, x.shape[:-1] + (w.n_out,))
+    return _run(_matvec, w.device, stream, w, x, out)
+
+
+def _matvec(st, w, x, out):
+    n_in, shape = w.n_in, x.shape[:-1] + (w.n_out,)
+    if x.dim() == 2 and x.stride(1) == 1 and x.stride(0) >= n_in:
+        m, step = x.shape[0], x.stride(0)
+    else:
+        x = x.reshape(-1, n_in).contiguous()
+        m, step = x.shape[0], n_in
+    if out is None:
+        out = x.new_empty(shape)
+    if m:
+        _raise(lib().ecasq_matvec(w.packed.data_ptr(), _HALF[w.dtype], w.n_out, n_in, w.group,
+                                  x.data_ptr(), m, step, st, out.data_ptr()))
     return out
 
 
@@ -605,6 +617,7 @@ class ecasq_kv_cache:
                              self.page_size, self.batch, self.max_pages, self.n_pages,
                              *[x.data_ptr() if x is not None else None for x in
                                (k, v, k_books, v_books, table, lens, mass, pos)])
+        self._ref = ctypes.byref(self._c)
         self._sizes = {}
 
     def __setattr__(self, name, value):
@@ -617,11 +630,11 @@ class ecasq_kv_cache:
         key = (name,) + args
         size = self._sizes.get(key)
         if size is None:
-            size = getattr(lib(), name)(ctypes.byref(self._c), *args)
+            size = getattr(lib(), name)(self._ref, *args)
             if size == 0:
                 raise EcasqError(ECASQ_EINVAL)
             self._sizes[key] = size
-        return torch.empty(size, dtype=torch.uint8, device=self.device), size
+        return self.table.new_empty(size, dtype=torch.uint8), size
 
 
 def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=None,
@@ -631,7 +644,7 @@ def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=
     already counts them.  A cache of symbols takes the rows' codebooks and counts
     as ecasq_solve_batched returns them for k.reshape(rows * heads, head_dim), and
     gives back the rounded rows in k_hat, v_hat where they are given."""
-    dev, inner = kv.device, kv.heads * kv.head_dim
+    dev = kv.device
     for name, x in (("k", k), ("v", v)):
         if not isinstance(x, torch.Tensor) or x.dtype != kv.dtype or x.device != dev:
             raise TypeError(f"{name} must be a {kv.dtype} tensor on {dev}")
@@ -656,17 +669,22 @@ def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=
                 _tensor(x, name, kv.dtype, dev, (rows, kv.heads, kv.head_dim))
     elif k_codebooks is not None or v_codebooks is not None:
         raise ValueError("a cache of rows takes no codebooks")
-    if rows == 0:
-        return
-    with _on(dev, stream) as st:
-        k, ks = _rows_apart(k, inner)
-        v, vs = _rows_apart(v, inner)
-        _raise(lib().ecasq_kv_write(ctypes.byref(kv._c), k.data_ptr(), ks, v.data_ptr(), vs, rows,
-                                    starts.data_ptr(),
-                                    positions.data_ptr() if positions is not None else None, st,
-                                    *books, s, int(seed) & (2 ** 64 - 1),
-                                    k_hat.data_ptr() if k_hat is not None else None,
-                                    v_hat.data_ptr() if v_hat is not None else None))
+    if rows:
+        _run(_write, dev, stream, kv, k, v, starts, positions, books, s,
+             int(seed) & (2 ** 64 - 1), k_hat, v_hat)
+
+
+def _write(st, kv, k, v, starts, positions, books, s, seed, k_hat, v_hat):
+    inner = kv.heads * kv.head_dim
+    rows = k.shape[0]
+    k, ks = _rows_apart(k, inner)
+    v, vs = _rows_apart(v, inner)
+    _raise(lib().ecasq_kv_write(kv._ref, k.data_ptr(), ks, v.data_ptr(), vs, rows,
+                                starts.data_ptr(),
+                                positions.data_ptr() if positions is not None else None, st,
+                                *books, s, seed,
+                                k_hat.data_ptr() if k_hat is not None else None,
+                                v_hat.data_ptr() if v_hat is not None else None))
 
 
 def ecasq_kv_attention(kv, q, scale=None, mass_out=None, out=None, stream=None):
@@ -678,21 +696,23 @@ def ecasq_kv_attention(kv, q, scale=None, mass_out=None, out=None, stream=None):
         raise TypeError(f"q must be a {kv.dtype} tensor on {kv.device}")
     if q.dim() != 3 or q.shape[0] != kv.batch or q.shape[2] != kv.head_dim:
         raise ValueError(f"q must be [{kv.batch}, q_heads, {kv.head_dim}]")
-    q_heads = q.shape[1]
     if mass_out is not None:
         _tensor(mass_out, "mass_out", torch.float32, kv.device, kv._slots_shape)
-    with _on(kv.device, stream) as st:
-        q, step = _rows_apart(q, q_heads * kv.head_dim)
-        if out is None:
-            out = torch.empty((kv.batch, q_heads, kv.head_dim), dtype=kv.dtype, device=kv.device)
-        else:
-            _tensor(out, "out", kv.dtype, kv.device, (kv.batch, q_heads, kv.head_dim))
-        ws, size = kv._workspace("ecasq_kv_attention_workspace", q_heads,
-                                 int(mass_out is not None))
-        _raise(lib().ecasq_kv_attention(ctypes.byref(kv._c), q.data_ptr(), step, q_heads,
-                                        kv.head_dim ** -0.5 if scale is None else float(scale),
-                                        mass_out.data_ptr() if mass_out is not None else None, st,
-                                        out.data_ptr(), ws.data_ptr(), size))
+    if out is not None:
+        _tensor(out, "out", kv.dtype, kv.device, q.shape)
+    return _run(_attention, kv.device, stream, kv, q, scale, mass_out, out)
+
+
+def _attention(st, kv, q, scale, mass_out, out):
+    q_heads = q.shape[1]
+    if out is None:
+        out = q.new_empty(q.shape)
+    q, step = _rows_apart(q, q_heads * kv.head_dim)
+    ws, size = kv._workspace("ecasq_kv_attention_workspace", q_heads, int(mass_out is not None))
+    _raise(lib().ecasq_kv_attention(kv._ref, q.data_ptr(), step, q_heads,
+                                    kv.head_dim ** -0.5 if scale is None else float(scale),
+                                    mass_out.data_ptr() if mass_out is not None else None, st,
+                                    out.data_ptr(), ws.data_ptr(), size))
     return out
 
 
@@ -709,12 +729,13 @@ def ecasq_kv_evict(kv, keep, recent=0, mass_out=None, pos_out=None, lens_out=Non
         _tensor(pos_out, "pos_out", torch.int32, kv.device, kv._slots_shape)
     lens_out = kv.lens if lens_out is None else \
         _tensor(lens_out, "lens_out", torch.int32, kv.device, (kv.batch,))
-    keep, recent = int(keep), int(recent)
-    with _on(kv.device, stream) as st:
-        ws, size = kv._workspace("ecasq_kv_evict_workspace", keep)
-        _raise(lib().ecasq_kv_evict(ctypes.byref(kv._c), keep, recent, mass_out.data_ptr(),
-                                    pos_out.data_ptr(), lens_out.data_ptr(), st, ws.data_ptr(),
-                                    size))
+    _run(_evict, kv.device, stream, kv, int(keep), int(recent), mass_out, pos_out, lens_out)
+
+
+def _evict(st, kv, keep, recent, mass_out, pos_out, lens_out):
+    ws, size = kv._workspace("ecasq_kv_evict_workspace", keep)
+    _raise(lib().ecasq_kv_evict(kv._ref, keep, recent, mass_out.data_ptr(), pos_out.data_ptr(),
+                                lens_out.data_ptr(), st, ws.data_ptr(), size))
 
 
 def infos_to_dicts(infos):
