@@ -395,7 +395,7 @@ ecasq_status ecasq_solve_batched(const void *x, ecasq_dtype dt, int64_t n, int64
  * against packed_bytes), 16-byte aligned.
  * ecasq_matvec: x, device, m rows of n_in entries x_stride >= n_in entries
  * apart, 1 <= m <= 2^20; y, device, m x n_out.  x and y need the alignment of
- * their type only.  The packed matrix is read once for every 64 rows of x.  No
+ * their type only.  The packed matrix is read once for every 16 rows of x.  No
  * workspace; results do not depend on the run or on m's other rows.  Both return
  * once the work is enqueued.
  */

@@ -1,4 +1,6 @@
 // Products with 4-bit weights: y[r][o] = sum_g s[o][g] sum_{i in g} c[sym[o][i]] x[r][i].
+#include <type_traits>
+
 #include "half16.hpp"
 #include "serve.hpp"
 
@@ -12,6 +14,11 @@ __global__ __launch_bounds__(256) void k_weights_pack(const uint8_t* __restrict_
                                                       const uint16_t* __restrict__ scales,
                                                       Weights w, char* __restrict__ packed) {
     const int64_t nw = w.tiles() * w.blocks() * 256, ns = w.tiles() * w.groups() * 16;
+    // What fills up tiles and blocks meets zeros of x and is not to make NaN of them: a
+    // symbol whose value is finite (0 if there is none).
+    uint32_t pad = 0;
+    for (int k = 15; k >= 0; k--)
+        if (k < t && __builtin_isfinite(from16<DT>(to16<DT>(cb[k])))) pad = (uint32_t)k;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < nw + ns + kWHead / 2;
          at += (int64_t)gridDim.x * 256) {
         if (at < nw) {
@@ -20,13 +27,14 @@ __global__ __launch_bounds__(256) void k_weights_pack(const uint8_t* __restrict_
             const int64_t o = block / w.blocks() * 16 + l % 16;
             const int64_t i0 = block % w.blocks() * 128 + 32 * j + 8 * (l / 16);
             uint32_t v = 0;
-            if (o < w.n_out) {
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if (i0 + i < w.n_in) {
-                        const uint32_t s = sym[o * w.n_in + i0 + i];
-                        v |= (s < (uint32_t)t ? s : (uint32_t)t - 1u) << (4 * i);
-                    }
+            for (int i = 0; i < 8; i++) {
+                uint32_t s = pad;
+                if (o < w.n_out && i0 + i < w.n_in) {
+                    s = sym[o * w.n_in + i0 + i];
+                    s = s < (uint32_t)t ? s : (uint32_t)t - 1u;
+                }
+                v |= s << (4 * i);
             }
             reinterpret_cast<uint32_t*>(packed + kWHead)[at] = v;
         } else if (at < nw + ns) {
@@ -40,14 +48,21 @@ __global__ __launch_bounds__(256) void k_weights_pack(const uint8_t* __restrict_
     }
 }
 
-// Products on the matrix cores, 16 rows of W by 16 NT rows of x per wavefront.  A
-// workgroup's 16 wavefronts take 16 / S tiles, S of them a part of the columns each,
-// and add their sums at the end.  Symbols become operands two at a time: a byte
-// selects its pair of values from a table of all 256 pairs in LDS, one dword each,
-// held in 64 copies so that every lane reads its own bank; the address is one byte
-// permutation (the byte above the lane's four).  A block's sums (fp32, exact
-// products) are multiplied by the scales of their rows as they leave the matrix
-// cores, STEP products of 32 columns at a time.
+// Products on the matrix cores, 16 rows of W (a tile) by up to 16 rows of x.  The
+// columns are cut into chunks of 128 NB (NB KB of a tile's symbols); S of a workgroup's
+// 16 wavefronts take the chunks of one tile, and go over their tiles with the next
+// chunk's symbols always on the way; their sums are added when a tile ends.  Up to
+// 8192 columns a wavefront has one chunk and reads its part of x once for all tiles:
+// loads return in order, so a wait for x was one for the symbols behind it (28672 x
+// 8192, one row of x: 41 us against 30).  Above, it has several, and reads its part of
+// x again for every `turns` tiles.
+//
+// Symbols become operands two at a time: a byte selects its pair of values from a
+// table of all 256 pairs in LDS, one dword each, held in 64 copies so that every
+// lane reads its own bank; the address is one byte permutation (the byte above the
+// lane's four).  Sums (fp32, exact products) are multiplied by the scales of their
+// rows as they leave the matrix cores, STEP products of 32 columns at a time.  What a
+// row of x gives depends on the matrix alone, not on the other rows.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
@@ -65,59 +80,110 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
                                                        __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
 }
 
-// The rows' scales of one tile and group for a lane's four results.
-template <int DT>
+// The scales of a lane's four results, of which lane `u` of each 16 has those of
+// product u (32 columns) of the chunk.
+template <int DT, int U>
 __device__ __forceinline__ f32x4 scales4(uint2 w) {
-    return f32x4{from16<DT>(w.x & 0xFFFFu), from16<DT>(w.x >> 16), from16<DT>(w.y & 0xFFFFu),
-                 from16<DT>(w.y >> 16)};
+    const uint32_t x = __builtin_amdgcn_update_dpp(0, (int)w.x, 0x150 + U, 0xF, 0xF, true);
+    const uint32_t y = __builtin_amdgcn_update_dpp(0, (int)w.y, 0x150 + U, 0xF, 0xF, true);
+    return f32x4{from16<DT>(x & 0xFFFFu), from16<DT>(x >> 16), from16<DT>(y & 0xFFFFu),
+                 from16<DT>(y >> 16)};
 }
 
 struct MatvecArgs {
     const char* packed;
     const uint16_t* x;
     uint16_t* y;
-    int64_t x_stride, n_out, tiles, scales_at;
-    int32_t n_in, m, blocks, groups;
-    int32_t unit, unit_shift;  // a group's products of 32 STEP columns; its log2, -1 if none
-    int32_t split_shift;       // log2 of S
+    int64_t x_stride, n_out, scales_at;
+    int32_t n_in, m, tiles, blocks, groups;
+    int32_t unit, unit_shift;  // products of 32 columns per group; its log2, -1 if none
+    int32_t parts;             // S
+    int32_t slots;             // tiles that a workgroup has at a time
+    int32_t turns;             // MANY: tiles for which a part of x is kept
 };
+constexpr int kTurns = 4;
 
-template <int DT, int NT, int STEP>
+// MANY: more chunks than wavefronts (then S is 16).
+template <int DT, int STEP, int NB, bool MANY>
 __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
-    __shared__ __align__(256) char lds[65536];
+    __shared__ __align__(256) char table[65536];
+    __shared__ float sums[MANY ? kTurns : 2][kMW * 256];
     const int lane = threadIdx.x % 64, n16 = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int S = 1 << p.split_shift, part = wave & (S - 1);
-    const int64_t tile = (int64_t)blockIdx.x * (kMW >> p.split_shift) + (wave >> p.split_shift);
-    const int32_t t0 = blockIdx.y * (16 * NT);
-    const bool live = tile < p.tiles;
-    const int32_t b0 = (int32_t)((int64_t)p.blocks * part >> p.split_shift);
-    const int32_t b1 = live ? (int32_t)((int64_t)p.blocks * (part + 1) >> p.split_shift) : b0;
-    const int32_t whole = p.n_in / 128 < b1 ? p.n_in / 128 : b1;  // blocks without padding
+    const int S = p.parts, slot = wave / S, part = wave - slot * S;
+    const int32_t t0 = blockIdx.y * 16, chunks = (p.blocks + NB - 1) / NB;
+    const int32_t turns = MANY ? p.turns : 1, stride = gridDim.x * p.slots * turns;
+    int32_t tile = blockIdx.x * p.slots * turns + slot;
+    const bool busy = slot < p.slots && part < chunks;
 
-    const char* words = p.packed + kWHead + (tile * p.blocks + b0) * 1024 + lane * 16;
-    const char* scales = p.packed + p.scales_at + tile * p.groups * 32 + g * 8;
-    u32x4 next = {0u, 0u, 0u, 0u};
-    if (b0 < b1) next = *reinterpret_cast<const u32x4*>(words);
+    // this lane's part of chunk c of tile t (the last tile's for those past it)
+    auto words_of = [&](int32_t t, int32_t c, int i) {
+        const int64_t row = t < p.tiles ? t : p.tiles - 1;
+        const int32_t b = NB * c + i < p.blocks ? NB * c + i : p.blocks - 1;
+        return *reinterpret_cast<const u32x4*>(p.packed + kWHead + (row * p.blocks + b) * 1024 +
+                                               lane * 16);
+    };
+    auto scales_of = [&](int32_t t, int32_t c) {
+        const int64_t row = t < p.tiles ? t : p.tiles - 1;
+        const int32_t u = 4 * NB * c + n16;
+        const int32_t k = p.unit_shift >= 0 ? u >> p.unit_shift : u / p.unit;
+        uint2 v = {0u, 0u};  // past the matrix: of x and of the symbols' values, which are 0 and finite
+        if (k < p.groups)
+            v = *reinterpret_cast<const uint2*>(p.packed + p.scales_at +
+                                                (row * p.groups + k) * 32 + g * 8);
+        return v;
+    };
+    u32x4 q[NB];
+    uint2 scale = {0u, 0u};
+    if (busy) {
+#pragma unroll
+        for (int i = 0; i < NB; i++) q[i] = words_of(tile, part, i);
+        scale = scales_of(tile, part);
+    }
 
+    // x of chunk c: entries of this lane's row, 0 past the matrix and past the rows
+    const bool has = t0 + n16 < p.m;
+    const uint16_t* xr = p.x + (int64_t)(has ? t0 + n16 : t0) * p.x_stride + 8 * g;
+    u32x4 x[4 * NB];
+    auto read_x = [&](int32_t c) {
+        const int32_t i0 = 128 * NB * c, left = p.n_in - i0;
+        if (left >= 128 * NB) {
+#pragma unroll
+            for (int k = 0; k < 4 * NB; k++) {
+                x[k] = u32x4{0u, 0u, 0u, 0u};
+                if (has) __builtin_memcpy(&x[k], xr + i0 + 32 * k, 16);
+            }
+            return;
+        }
+        // the product that the matrix ends in, entry by entry
+        u32x4 edge = {0u, 0u, 0u, 0u};
+        const int32_t e0 = i0 + left / 32 * 32;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const bool in = has && e0 + 8 * g + e < p.n_in;
+            const uint32_t v = in ? xr[e0 + e] : 0u;
+            edge[e / 2] |= v << (e % 2 * 16);
+        }
+#pragma unroll
+        for (int k = 0; k < 4 * NB; k++) {
+            x[k] = u32x4{0u, 0u, 0u, 0u};
+            if (32 * (k + 1) <= left) {
+                if (has) __builtin_memcpy(&x[k], xr + i0 + 32 * k, 16);
+            } else if (32 * k < left) {
+                x[k] = edge;
+            }
+        }
+    };
+    if (!MANY && busy) read_x(part);
     {  // the table: pair e, copy k at 256 e + 4 k
         const uint16_t* cb = reinterpret_cast<const uint16_t*>(p.packed);
         const uint32_t lo = cb[threadIdx.x / 16 % 16];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const uint32_t v = lo | (uint32_t)cb[4 * i + threadIdx.x / 256] << 16;
-            *reinterpret_cast<u32x4*>(lds + i * 16384 + threadIdx.x * 16) = u32x4{v, v, v, v};
+            *reinterpret_cast<u32x4*>(table + i * 16384 + threadIdx.x * 16) = u32x4{v, v, v, v};
         }
     }
-    const uint16_t* xs[NT];
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const int32_t r = t0 + 16 * t + n16;
-        xs[t] = p.x + (int64_t)(r < p.m ? r : p.m - 1) * p.x_stride + 8 * g;
-    }
-    f32x4 total[NT];
-#pragma unroll
-    for (int t = 0; t < NT; t++) total[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     __syncthreads();
 
     const uint32_t at = 4 * lane;
@@ -126,91 +192,92 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
 #pragma unroll
         for (int k = 0; k < 4; k++)
             a[k] = *reinterpret_cast<const uint32_t*>(
-                lds + __builtin_amdgcn_perm(w, at, 0x0C0C0000u | (uint32_t)(4 + k) << 8));
+                table + __builtin_amdgcn_perm(w, at, 0x0C0C0000u | (uint32_t)(4 + k) << 8));
         return a;
     };
-    auto group_of = [&](int32_t u) {  // of unit u of 32 STEP columns
-        return p.unit_shift >= 0 ? u >> p.unit_shift : u / p.unit;
+    // the symbols q, with the scales `scale`, of chunk c; the next to come are those of tile2, c2
+    auto chunk = [&](auto WHOLE, int32_t c, int32_t tile2, int32_t c2) {
+        f32x4 total = {0.0f, 0.0f, 0.0f, 0.0f};
+        const uint2 scale2 = scales_of(tile2, c2);
+        auto block = [&](auto I) {
+            constexpr int i = decltype(I)::value;
+            if (WHOLE.value || NB * c + i < p.blocks) {
+                f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+                auto product = [&](auto J) {
+                    constexpr int j = decltype(J)::value;
+                    sum = mfma<DT>(operand(q[i][j]), x[4 * i + j], sum);
+                    if (STEP == 1 || j == 3) {
+                        const f32x4 s = scales4<DT, 4 * i + (STEP == 1 ? j : 0)>(scale);
+#pragma unroll
+                        for (int k = 0; k < 4; k++)
+                            total[k] = __builtin_fmaf(s[k], sum[k], total[k]);
+                        sum = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    }
+                };
+                product(std::integral_constant<int, 0>{});
+                product(std::integral_constant<int, 1>{});
+                product(std::integral_constant<int, 2>{});
+                product(std::integral_constant<int, 3>{});
+            }
+            q[i] = words_of(tile2, c2, i);
+        };
+        block(std::integral_constant<int, 0>{});
+        if constexpr (NB > 1) block(std::integral_constant<int, 1>{});
+        if constexpr (NB > 2) block(std::integral_constant<int, 2>{});
+        if constexpr (NB > 3) block(std::integral_constant<int, 3>{});
+        scale = scale2;
+        return total;
+    };
+    auto either = [&](int32_t c, int32_t tile2, int32_t c2) {
+        return 128 * NB * (c + 1) <= p.n_in ? chunk(std::true_type{}, c, tile2, c2)
+                                            : chunk(std::false_type{}, c, tile2, c2);
     };
 
-    for (int32_t b = b0; b < whole; b++) {
-        const u32x4 now = next;
-        words += 1024;
-        if (b + 1 < b1) next = *reinterpret_cast<const u32x4*>(words);
-        uint2 sw[4 / STEP];
-#pragma unroll
-        for (int u = 0; u < 4 / STEP; u++)
-            sw[u] = *reinterpret_cast<const uint2*>(
-                scales + (int64_t)group_of(b * (4 / STEP) + u) * 32);
-        u32x4 xv[NT][4];
-#pragma unroll
-        for (int t = 0; t < NT; t++)
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-                __builtin_memcpy(&xv[t][j], xs[t] + (int64_t)b * 128 + 32 * j, 16);
-#pragma unroll
-        for (int u = 0; u < 4 / STEP; u++) {
-            f32x4 sum[NT];
-#pragma unroll
-            for (int t = 0; t < NT; t++) sum[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int j = u * STEP; j < (u + 1) * STEP; j++) {
-                const u32x4 a = operand(now[j]);
-#pragma unroll
-                for (int t = 0; t < NT; t++) sum[t] = mfma<DT>(a, xv[t][j], sum[t]);
-            }
-            const f32x4 s = scales4<DT>(sw[u]);
-#pragma unroll
-            for (int t = 0; t < NT; t++)
-#pragma unroll
-                for (int r = 0; r < 4; r++)
-                    total[t][r] = __builtin_fmaf(s[r], sum[t][r], total[t][r]);
-        }
-    }
-    if (whole < b1 && b0 < b1) {  // the last block, with columns past the matrix: both operands 0 there
-        const int32_t i0 = (b1 - 1) * 128;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int32_t i = i0 + 32 * j;
-            if (i >= p.n_in) break;
-            u32x4 a = operand(next[j]);
-#pragma unroll
-            for (int k = 0; k < 8; k++)
-                if (i + 8 * g + k >= p.n_in) a[k / 2] &= k % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-            const f32x4 s = scales4<DT>(*reinterpret_cast<const uint2*>(
-                scales + (int64_t)group_of(i / (32 * STEP)) * 32));
-#pragma unroll
-            for (int t = 0; t < NT; t++) {
-                u32x4 xv = {0u, 0u, 0u, 0u};
-#pragma unroll
-                for (int k = 0; k < 8; k++)
-                    if (i + 8 * g + k < p.n_in)
-                        xv[k / 2] |= (uint32_t)xs[t][i + k] << (k % 2 * 16);
-                const f32x4 sum = mfma<DT>(a, xv, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-#pragma unroll
-                for (int r = 0; r < 4; r++) total[t][r] = __builtin_fmaf(s[r], sum[r], total[t][r]);
-            }
-        }
-    }
-
-    // sums of the S parts in order; result r of lane l of part w at 256 (w NT + t) + 64 r + l
-    __syncthreads();
-    float* sums = reinterpret_cast<float*>(lds);
-#pragma unroll
-    for (int t = 0; t < NT; t++)
-#pragma unroll
-        for (int r = 0; r < 4; r++) sums[(wave * NT + t) * 256 + 64 * r + lane] = total[t][r];
-    __syncthreads();
-    if (!live) return;
-    const float* mine = sums + (wave - part) * NT * 256;
-    for (int k = part * 64 + lane; k < NT * 256; k += S * 64) {
-        const int row = k % 16, col = k / 16 % 16, t = k / 256;
-        const float* from = mine + t * 256 + row % 4 * 64 + row / 4 * 16 + col;
+    // result k of lane l of wavefront w at 256 w + 64 k + l of its tile's sums
+    auto finish = [&](const float* mine, int32_t t, int k) {
+        const int row = k % 16, col = k / 16;
+        const float* from = mine + row % 4 * 64 + row / 4 * 16 + col;
         float v = from[0];
-        for (int w = 1; w < S; w++) v += from[w * NT * 256];
-        const int64_t o = tile * 16 + row;
-        const int32_t r = t0 + 16 * t + col;
-        if (o < p.n_out && r < p.m) p.y[(int64_t)r * p.n_out + o] = to16<DT>(v);
+        for (int w = 1; w < S; w++) v += from[w * 256];
+        const int64_t o = (int64_t)t * 16 + row;
+        if (t < p.tiles && o < p.n_out && t0 + col < p.m)
+            p.y[(int64_t)(t0 + col) * p.n_out + o] = to16<DT>(v);
+    };
+    const int32_t begin = blockIdx.x * p.slots * turns;
+    if constexpr (!MANY) {
+        int turn = 0;
+        for (int32_t first = begin; first < p.tiles; first += stride) {
+            if (busy) {
+                const f32x4 total = either(part, tile + stride, part);
+#pragma unroll
+                for (int k = 0; k < 4; k++) sums[turn][wave * 256 + 64 * k + lane] = total[k];
+            }
+            __syncthreads();
+            if (slot < p.slots)
+                for (int k = part * 64 + lane; k < 256; k += S * 64)
+                    finish(sums[turn] + slot * S * 256, tile, k);
+            turn ^= 1;  // (the next sums go where nobody reads)
+            tile += stride;
+        }
+    } else {
+        for (int32_t first = begin; first < p.tiles; first += stride) {
+            for (int32_t c = part; c < chunks; c += kMW) {
+                read_x(c);
+                for (int t = 0; t < turns; t++) {
+                    const bool end = t + 1 == turns, last = end && c + kMW >= chunks;
+                    const f32x4 total = either(c, last ? first + stride : first + (end ? 0 : t + 1),
+                                               last ? part : end ? c + kMW : c);
+                    float* to = sums[t] + wave * 256 + lane;
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+                        to[64 * k] = c == part ? total[k] : to[64 * k] + total[k];
+                }
+            }
+            __syncthreads();
+            for (int k = threadIdx.x; k < turns * 256; k += kMT)
+                finish(sums[k / 256], first + k / 256, k % 256);
+            __syncthreads();
+        }
     }
 }
 
@@ -231,22 +298,19 @@ hipError_t launch_weights_pack(const uint8_t* symbols, const double* codebook, i
 
 namespace {
 
-template <int DT, int NT>
-void matvec_step(const MatvecArgs& a, int step, dim3 g, hipStream_t st) {
-    if (step == 4)
-        k_matvec<DT, NT, 4><<<g, kMT, 0, st>>>(a);
-    else
-        k_matvec<DT, NT, 1><<<g, kMT, 0, st>>>(a);
-}
-
-template <int DT>
-void matvec_rows(const MatvecArgs& a, int nt, int step, dim3 g, hipStream_t st) {
-    if (nt == 1)
-        matvec_step<DT, 1>(a, step, g, st);
-    else if (nt == 2)
-        matvec_step<DT, 2>(a, step, g, st);
-    else
-        matvec_step<DT, 4>(a, step, g, st);
+template <int NB, bool MANY>
+void matvec_go(const MatvecArgs& a, int dt, int step, dim3 g, hipStream_t st) {
+    if (dt == ECASQ_F16) {
+        if (step == 4)
+            k_matvec<1, 4, NB, MANY><<<g, kMT, 0, st>>>(a);
+        else
+            k_matvec<1, 1, NB, MANY><<<g, kMT, 0, st>>>(a);
+    } else {
+        if (step == 4)
+            k_matvec<2, 4, NB, MANY><<<g, kMT, 0, st>>>(a);
+        else
+            k_matvec<2, 1, NB, MANY><<<g, kMT, 0, st>>>(a);
+    }
 }
 
 }  // namespace
@@ -261,25 +325,46 @@ hipError_t launch_matvec(const char* packed, int dt, const Weights& w, const voi
     a.n_out = w.n_out;
     a.n_in = (int32_t)w.n_in;
     a.m = (int32_t)m;
-    a.tiles = w.tiles();
+    a.tiles = (int32_t)w.tiles();
     a.blocks = (int32_t)w.blocks();
     a.groups = (int32_t)w.groups();
     a.scales_at = w.scales_at();
+    a.unit = (int32_t)(w.group / 32);
+    a.unit_shift = (a.unit & (a.unit - 1)) == 0 ? __builtin_ctz((unsigned)a.unit) : -1;
     // scales change at whole blocks of 128 columns, or anywhere between products of 32
     const int step = w.group % 128 == 0 ? 4 : 1;
-    a.unit = (int32_t)(w.group / (32 * step));
-    a.unit_shift = (a.unit & (a.unit - 1)) == 0 ? __builtin_ctz((unsigned)a.unit) : -1;
-    // parts of the columns: until there are 4096 wavefronts, 16 for each CU
-    while (a.split_shift < 4 && (a.tiles << a.split_shift) < 4096 &&
-           (2 << a.split_shift) <= a.blocks)
-        a.split_shift++;
-    const int nt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-    const int64_t per = kMW >> a.split_shift;
-    const dim3 g((unsigned)((a.tiles + per - 1) / per), (unsigned)((m + 16 * nt - 1) / (16 * nt)));
-    if (dt == ECASQ_F16)
-        matvec_rows<1>(a, nt, step, g, st);
+
+    // A workgroup per CU.  Chunks of nb blocks give every tile S wavefronts and a
+    // workgroup 16 / S tiles; a round takes about nb and as much as a block for its end.
+    constexpr int32_t cus = 256;
+    int32_t nb = 4, least = INT32_MAX;
+    const bool many = a.blocks > 4 * kMW;
+    for (int32_t k = 1; !many && k <= 4; k++) {
+        const int32_t parts = (a.blocks + k - 1) / k;
+        if (parts > kMW) continue;
+        const int32_t at_once = cus * (kMW / parts);
+        const int32_t cost = (a.tiles + at_once - 1) / at_once * (k + 1);
+        if (cost < least) {
+            least = cost;
+            nb = k;
+        }
+    }
+    a.parts = many ? kMW : (a.blocks + nb - 1) / nb;
+    a.slots = (a.tiles + cus - 1) / cus;
+    a.turns = many ? (a.slots < kTurns ? a.slots : kTurns) : 1;
+    if (a.slots > kMW / a.parts) a.slots = kMW / a.parts;
+    const int32_t each = a.slots * a.turns, wgs = (a.tiles + each - 1) / each;
+    const dim3 g((unsigned)(wgs < cus ? wgs : cus), (unsigned)((m + 15) / 16));
+    if (many)
+        matvec_go<4, true>(a, dt, step, g, st);
+    else if (nb == 1)
+        matvec_go<1, false>(a, dt, step, g, st);
+    else if (nb == 2)
+        matvec_go<2, false>(a, dt, step, g, st);
+    else if (nb == 3)
+        matvec_go<3, false>(a, dt, step, g, st);
     else
-        matvec_rows<2>(a, nt, step, g, st);
+        matvec_go<4, false>(a, dt, step, g, st);
     return hipGetLastError();
 }
 

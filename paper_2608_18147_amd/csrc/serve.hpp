@@ -14,7 +14,8 @@ namespace ecasq {
 // every tile of 16 rows and block of 128 columns 1024 bytes of symbols, 16
 // for each lane l = (row l % 16, quarter q = l / 16): dword j holds columns 32 j +
 // 8 q + i, i = 0 .. 7, at bits 4 i; then for every tile and group the 16 rows'
-// scales.  Rows and columns past the matrix hold symbol 0 and scale 0.
+// scales.  Rows and columns past the matrix hold the first symbol of a finite value and
+// scale 0.
 constexpr int64_t kWHead = 256;
 struct Weights {
     int64_t n_out, n_in, group;
