@@ -54,8 +54,10 @@ __global__ __launch_bounds__(256) void k_weights_pack(const uint8_t* __restrict_
 // chunk's symbols always on the way; their sums are added when a tile ends.  Up to
 // 8192 columns a wavefront has one chunk and reads its part of x once for all tiles:
 // loads return in order, so a wait for x was one for the symbols behind it (28672 x
-// 8192, one row of x: 41 us against 30).  Above, it has several, and reads its part of
-// x again for every `turns` tiles.
+// 8192, one row of x: 41 us against 30).  Above, it has several; the rows of x are then
+// in LDS where they fit (28672 columns for one row, 14336 for two), or a part of x is
+// read again for every `turns` tiles (8192 x 28672, one row: 28 us by the first, 32 by the
+// second).
 //
 // Symbols become operands two at a time: a byte selects its pair of values from a
 // table of all 256 pairs in LDS, one dword each, held in 64 copies so that every
@@ -101,18 +103,22 @@ struct MatvecArgs {
     int32_t slots;             // tiles that a workgroup has at a time
     int32_t turns;             // MANY: tiles for which a part of x is kept
 };
-constexpr int kTurns = 4;
+constexpr int kTurns = 4, kXBytes = 65536;
 
-// MANY: more chunks than wavefronts (then S is 16).
-template <int DT, int STEP, int NB, bool MANY>
+// A wavefront has one chunk; or several (then S is 16 and a workgroup has one tile at a
+// time), with x in registers or in LDS.
+enum Mode { kOne, kMany, kManyLds };
+
+template <int DT, int STEP, int NB, int MODE>
 __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
     __shared__ __align__(256) char table[65536];
-    __shared__ float sums[MANY ? kTurns : 2][kMW * 256];
+    __shared__ float sums[MODE == kMany ? kTurns : 2][kMW * 256];
+    __shared__ __align__(16) char xlds[MODE == kManyLds ? kXBytes : 16];
     const int lane = threadIdx.x % 64, n16 = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int S = p.parts, slot = wave / S, part = wave - slot * S;
     const int32_t t0 = blockIdx.y * 16, chunks = (p.blocks + NB - 1) / NB;
-    const int32_t turns = MANY ? p.turns : 1, stride = gridDim.x * p.slots * turns;
+    const int32_t turns = MODE == kMany ? p.turns : 1, stride = gridDim.x * p.slots * turns;
     int32_t tile = blockIdx.x * p.slots * turns + slot;
     const bool busy = slot < p.slots && part < chunks;
 
@@ -144,7 +150,7 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
     // x of chunk c: entries of this lane's row, 0 past the matrix and past the rows
     const bool has = t0 + n16 < p.m;
     const uint16_t* xr = p.x + (int64_t)(has ? t0 + n16 : t0) * p.x_stride + 8 * g;
-    u32x4 x[4 * NB];
+    u32x4 x[MODE == kManyLds ? 1 : 4 * NB];
     auto read_x = [&](int32_t c) {
         const int32_t i0 = 128 * NB * c, left = p.n_in - i0;
         if (left >= 128 * NB) {
@@ -174,7 +180,25 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
             }
         }
     };
-    if (!MANY && busy) read_x(part);
+    if constexpr (MODE == kOne) {
+        if (busy) read_x(part);
+    }
+    const int32_t x_bytes = chunks * 256 * NB + 16;  // of a row in LDS
+    const char* x_row = xlds + (has ? n16 * x_bytes : 0) + 16 * g;
+    if constexpr (MODE == kManyLds) {
+        const int32_t rows = p.m - t0 < 16 ? p.m - t0 : 16, per = chunks * 16 * NB;
+        for (int32_t k = threadIdx.x; k < rows * per; k += kMT) {
+            const int32_t r = k / per, i = k % per * 8;
+            const uint16_t* from = p.x + (int64_t)(t0 + r) * p.x_stride;
+            u32x4 v = {0u, 0u, 0u, 0u};
+            if (i + 8 <= p.n_in)
+                __builtin_memcpy(&v, from + i, 16);
+            else
+                for (int e = 0; e < 8; e++)
+                    if (i + e < p.n_in) v[e / 2] |= (uint32_t)from[i + e] << (e % 2 * 16);
+            *reinterpret_cast<u32x4*>(xlds + r * x_bytes + 2 * i) = v;
+        }
+    }
     {  // the table: pair e, copy k at 256 e + 4 k
         const uint16_t* cb = reinterpret_cast<const uint16_t*>(p.packed);
         const uint32_t lo = cb[threadIdx.x / 16 % 16];
@@ -205,7 +229,12 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
                 f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
                 auto product = [&](auto J) {
                     constexpr int j = decltype(J)::value;
-                    sum = mfma<DT>(operand(q[i][j]), x[4 * i + j], sum);
+                    u32x4 v;
+                    if constexpr (MODE == kManyLds)
+                        v = *reinterpret_cast<const u32x4*>(x_row + 256 * (NB * c + i) + 64 * j);
+                    else
+                        v = x[4 * i + j];
+                    sum = mfma<DT>(operand(q[i][j]), v, sum);
                     if (STEP == 1 || j == 3) {
                         const f32x4 s = scales4<DT, 4 * i + (STEP == 1 ? j : 0)>(scale);
 #pragma unroll
@@ -244,11 +273,20 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
             p.y[(int64_t)(t0 + col) * p.n_out + o] = to16<DT>(v);
     };
     const int32_t begin = blockIdx.x * p.slots * turns;
-    if constexpr (!MANY) {
+    if constexpr (MODE != kMany) {
         int turn = 0;
         for (int32_t first = begin; first < p.tiles; first += stride) {
             if (busy) {
-                const f32x4 total = either(part, tile + stride, part);
+                f32x4 total;
+                if constexpr (MODE == kOne)
+                    total = either(part, tile + stride, part);
+                else
+                    for (int32_t c = part; c < chunks; c += kMW) {
+                        const bool last = c + kMW >= chunks;
+                        const f32x4 v =
+                            either(c, last ? tile + stride : tile, last ? part : c + kMW);
+                        total = c == part ? v : total + v;
+                    }
 #pragma unroll
                 for (int k = 0; k < 4; k++) sums[turn][wave * 256 + 64 * k + lane] = total[k];
             }
@@ -298,18 +336,18 @@ hipError_t launch_weights_pack(const uint8_t* symbols, const double* codebook, i
 
 namespace {
 
-template <int NB, bool MANY>
+template <int NB, int MODE>
 void matvec_go(const MatvecArgs& a, int dt, int step, dim3 g, hipStream_t st) {
     if (dt == ECASQ_F16) {
         if (step == 4)
-            k_matvec<1, 4, NB, MANY><<<g, kMT, 0, st>>>(a);
+            k_matvec<1, 4, NB, MODE><<<g, kMT, 0, st>>>(a);
         else
-            k_matvec<1, 1, NB, MANY><<<g, kMT, 0, st>>>(a);
+            k_matvec<1, 1, NB, MODE><<<g, kMT, 0, st>>>(a);
     } else {
         if (step == 4)
-            k_matvec<2, 4, NB, MANY><<<g, kMT, 0, st>>>(a);
+            k_matvec<2, 4, NB, MODE><<<g, kMT, 0, st>>>(a);
         else
-            k_matvec<2, 1, NB, MANY><<<g, kMT, 0, st>>>(a);
+            k_matvec<2, 1, NB, MODE><<<g, kMT, 0, st>>>(a);
     }
 }
 
@@ -335,7 +373,10 @@ hipError_t launch_matvec(const char* packed, int dt, const Weights& w, const voi
     const int step = w.group % 128 == 0 ? 4 : 1;
 
     // A workgroup per CU.  Chunks of nb blocks give every tile S wavefronts and a
-    // workgroup 16 / S tiles; a round takes about nb and as much as a block for its end.
+    // workgroup 16 / S tiles; a round takes about nb and as much as a block for its end.  Larger
+    // chunks where they save a fifth, since the tiles of a workgroup read x each for itself
+    // (14336 x 4096 for 16 rows: 14 us with 2 blocks, 17 with 4; 32124 x 1091 for 3: 15 with
+    // 1, 11 with 2).
     constexpr int32_t cus = 256;
     int32_t nb = 4, least = INT32_MAX;
     const bool many = a.blocks > 4 * kMW;
@@ -344,27 +385,30 @@ hipError_t launch_matvec(const char* packed, int dt, const Weights& w, const voi
         if (parts > kMW) continue;
         const int32_t at_once = cus * (kMW / parts);
         const int32_t cost = (a.tiles + at_once - 1) / at_once * (k + 1);
-        if (cost < least) {
+        if (least == INT32_MAX || 5 * (int64_t)cost < 4 * (int64_t)least) {
             least = cost;
             nb = k;
         }
     }
     a.parts = many ? kMW : (a.blocks + nb - 1) / nb;
     a.slots = (a.tiles + cus - 1) / cus;
-    a.turns = many ? (a.slots < kTurns ? a.slots : kTurns) : 1;
+    const bool in_lds = many && (m < 16 ? m : 16) * ((a.blocks + 3) / 4 * 1024 + 16) <= kXBytes;
+    a.turns = !many || in_lds ? 1 : a.slots < kTurns ? a.slots : kTurns;
     if (a.slots > kMW / a.parts) a.slots = kMW / a.parts;
     const int32_t each = a.slots * a.turns, wgs = (a.tiles + each - 1) / each;
     const dim3 g((unsigned)(wgs < cus ? wgs : cus), (unsigned)((m + 15) / 16));
-    if (many)
-        matvec_go<4, true>(a, dt, step, g, st);
+    if (in_lds)
+        matvec_go<4, kManyLds>(a, dt, step, g, st);
+    else if (many)
+        matvec_go<4, kMany>(a, dt, step, g, st);
     else if (nb == 1)
-        matvec_go<1, false>(a, dt, step, g, st);
+        matvec_go<1, kOne>(a, dt, step, g, st);
     else if (nb == 2)
-        matvec_go<2, false>(a, dt, step, g, st);
+        matvec_go<2, kOne>(a, dt, step, g, st);
     else if (nb == 3)
-        matvec_go<3, false>(a, dt, step, g, st);
+        matvec_go<3, kOne>(a, dt, step, g, st);
     else
-        matvec_go<4, false>(a, dt, step, g, st);
+        matvec_go<4, kOne>(a, dt, step, g, st);
     return hipGetLastError();
 }
 
