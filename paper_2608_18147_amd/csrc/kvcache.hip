@@ -120,127 +120,278 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int32_t pos, int64_t n
     return (b >> 31) ? ~b : b | 0x80000000u;
 }
 
-// Sum over the workgroup, the same for every thread.
-__device__ __forceinline__ int32_t block_count(int32_t v, int32_t* red) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
-    __syncthreads();
-    int32_t s = 0;
-    for (int k = 0; k < kET / 64; k++) s += red[k];
-    return s;
+// Inclusive sums over a wavefront: within rows of 16 lanes, then over the rows.
+__device__ __forceinline__ int32_t wave_sums(int32_t v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    return v;
 }
 
-// Exclusive prefix count of `on` over the workgroup's threads, and the total.
-__device__ __forceinline__ int32_t block_rank(bool on, int32_t* red, int32_t& total) {
-    const uint64_t m = __ballot(on);
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    __syncthreads();
-    if (lane == 0) red[wave] = __popcll(m);
-    __syncthreads();
-    int32_t before = 0, all = 0;
-    for (int k = 0; k < kET / 64; k++) {
-        if (k < wave) before += red[k];
-        all += red[k];
-    }
-    total = all;
-    return before + __popcll(m & ((1ull << lane) - 1));
-}
+// The workgroup's hold on one head's keys: every wavefront has a span of consecutive
+// slots, 64 at a time, so that ranks in slot order are a ballot's and three barriers'
+// work.  The keys are in LDS (KEYS of them; in registers, 32 to a thread, the unrolled
+// passes took 17 us for the shortest heads); longer heads (KEYS = 0) read mass and pos
+// again for every pass.  What is bounded by one CU's instructions for a long head is
+// bounded by the passes' latencies for a short one (FIXME).
+constexpr int kEW = kET / 64, kBins = 2048;
+constexpr int kKeysFew = 4096, kKeysMany = 32768;
 
-// A workgroup per sequence and head: the rank of the last kept slot by bisection
-// over the keys' bits, then the lists of freed and moving slots, then the moves.
-__global__ __launch_bounds__(kET) void k_kv_evict(ecasq_kv_cache c, int32_t keep, int32_t recent,
-                                                  float* mass_out, int32_t* pos_out,
-                                                  int32_t* __restrict__ lists) {
-    __shared__ int32_t red[kET / 64];
+struct EvictPlan {
+    int32_t keep, recent, moves;  // moves: the most a head can make
+    int32_t* lists;               // per head: freed slots, then moving ones, `moves` each
+    int32_t* counts;              // per head: moves made
+};
+
+template <int KEYS>
+__global__ __launch_bounds__(kET) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
+                                                  float* __restrict__ mass_out,
+                                                  int32_t* __restrict__ pos_out) {
     __shared__ int32_t newest;
-    const int32_t b = blockIdx.x / c.heads, head = blockIdx.x % c.heads;
-    const int64_t slots = kv_slots(c), n = kv_len(c, b);
-    const int64_t base = ((int64_t)b * c.heads + head) * slots;
+    __shared__ uint32_t hist[3][kBins];
+    __shared__ int32_t sums[3][kEW];
+    __shared__ int32_t found[3][2];
+    __shared__ int4 counts[kEW];
+    __shared__ uint32_t keys[KEYS ? KEYS : 1];
+    const int32_t b = blockIdx.x / c.heads;
+    const int32_t slots = (int32_t)kv_slots(c), n = (int32_t)kv_len(c, b), keep = e.keep;
+    const int64_t base = (int64_t)blockIdx.x * slots;
+    // (these may be c.mass and c.pos; nothing is read again after it is written)
     const float* mass = c.mass + base;
     const int32_t* pos = c.pos + base;
-    if (threadIdx.x == 0) newest = INT32_MIN;
-    __syncthreads();
-    const int64_t most = n < keep ? n : keep;
-    if (n > keep) {
-        int32_t p = INT32_MIN;
-        for (int64_t i = threadIdx.x; i < n; i += kET) p = max(p, pos[i]);
-        atomicMax(&newest, p);
-        __syncthreads();
-        const int64_t but = (int64_t)newest - recent;
-        // the largest key T with at least keep keys at or above it
-        uint32_t T = 0;
-        for (int bit = 31; bit >= 0; bit--) {
-            const uint32_t at = T | (1u << bit);
-            int32_t k = 0;
-            for (int64_t i = threadIdx.x; i < n; i += kET) k += evict_key(mass[i], pos[i], but) >= at;
-            if (block_count(k, red) >= keep) T = at;
-        }
-        int32_t above = 0;
-        for (int64_t i = threadIdx.x; i < n; i += kET) above += evict_key(mass[i], pos[i], but) > T;
-        int32_t ties = keep - block_count(above, red);  // slots of key T that are kept
-        int32_t* freed = lists + (int64_t)blockIdx.x * 2 * keep;
-        int32_t* moving = freed + keep;
-        int32_t nf = 0, nm = 0;
-        for (int64_t i0 = 0; i0 < n; i0 += kET) {
-            const int64_t i = i0 + threadIdx.x;
-            const uint32_t key = i < n ? evict_key(mass[i], pos[i], but) : 0u;
-            int32_t got = 0;
-            const bool tie = i < n && key == T;
-            const int32_t place = block_rank(tie, red, got);
-            const bool kept = i < n && (key > T || (tie && place < ties));
-            ties = max(0, ties - got);
-            const bool fr = i < keep && !kept, mv = i >= keep && kept;
-            int32_t at = block_rank(fr, red, got);
-            if (fr) freed[nf + at] = (int32_t)i;
-            nf += got;
-            at = block_rank(mv, red, got);
-            if (mv) moving[nm + at] = (int32_t)i;
-            nm += got;
-        }
-        __syncthreads();
-        // the moves: a wavefront each
-        const int lane = threadIdx.x % 64;
-        const int32_t row16 = c.coded ? c.head_dim / 32 : c.head_dim / 8;
-        for (int32_t m = threadIdx.x / 64; m < nf; m += kET / 64) {
-            const int64_t to = kv_row(c, b, head, freed[m]), from = kv_row(c, b, head, moving[m]);
-            if (to < 0 || from < 0) continue;
-            for (int e = lane; e < row16; e += 64) {
-                static_cast<uint4*>(c.k)[to * row16 + e] =
-                    static_cast<const uint4*>(c.k)[from * row16 + e];
-                static_cast<uint4*>(c.v)[to * row16 + e] =
-                    static_cast<const uint4*>(c.v)[from * row16 + e];
-            }
-            if (c.coded && lane < 4) {
-                uint4* books = static_cast<uint4*>(lane < 2 ? c.k_books : c.v_books);
-                books[to * 2 + lane % 2] = books[from * 2 + lane % 2];
-            }
-        }
-        __syncthreads();
-        if (mass_out != c.mass)
-            for (int64_t i = threadIdx.x; i < most; i += kET) mass_out[base + i] = mass[i];
-        if (pos_out != c.pos)
-            for (int64_t i = threadIdx.x; i < most; i += kET) pos_out[base + i] = pos[i];
-        __syncthreads();
-        for (int32_t m = threadIdx.x; m < nf; m += kET) {
-            mass_out[base + freed[m]] = mass[moving[m]];
-            pos_out[base + freed[m]] = pos[moving[m]];
-        }
+    mass_out += base;
+    pos_out += base;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (n <= keep) {
+        if (mass_out != mass)
+            for (int32_t i = threadIdx.x; i < n; i += kET) mass_out[i] = mass[i];
+        if (pos_out != pos)
+            for (int32_t i = threadIdx.x; i < n; i += kET) pos_out[i] = pos[i];
+        if (threadIdx.x == 0) e.counts[blockIdx.x] = 0;
         return;
     }
-    for (int64_t i = threadIdx.x; i < most; i += kET) {
-        mass_out[base + i] = mass[i];
-        pos_out[base + i] = pos[i];
+    const int32_t rounds = (n + kET - 1) / kET, first = wave * rounds * 64 + lane;
+    int32_t top = INT32_MIN;
+    if (threadIdx.x == 0) newest = INT32_MIN;
+    for (int k = threadIdx.x; k < 3 * kBins; k += kET) hist[0][k] = 0u;
+    // All of mass and pos at once; slots below keep go to the outputs as they are (the moves
+    // overwrite the freed ones).
+    constexpr int kHeld = KEYS / kET;
+    float m[KEYS ? kHeld : 1];
+    const bool copy_mass = mass_out != mass, copy_pos = pos_out != pos;
+    if constexpr (KEYS > 0) {
+        int32_t p[kHeld];
+#pragma unroll
+        for (int r = 0; r < kHeld; r++) {
+            const int32_t i = first + 64 * r;
+            m[r] = 0.0f;
+            p[r] = INT32_MIN;
+            if (r < rounds && i < n) {
+                m[r] = mass[i];
+                p[r] = pos[i];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kHeld; r++) {
+            const int32_t i = first + 64 * r;
+            if (r < rounds && i < n) {
+                keys[i] = (uint32_t)p[r];
+                top = max(top, p[r]);
+                if (copy_mass && i < keep) mass_out[i] = m[r];
+                if (copy_pos && i < keep) pos_out[i] = p[r];
+            }
+        }
+    } else {
+#pragma unroll 8
+        for (int32_t r = 0; r < rounds; r++) {
+            const int32_t i = first + 64 * r;
+            if (i < n) {
+                const int32_t v = pos[i];
+                top = max(top, v);
+                if (copy_mass && i < keep) mass_out[i] = mass[i];
+                if (copy_pos && i < keep) pos_out[i] = v;
+            }
+        }
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = max(top, __shfl_xor(top, off));
+    __syncthreads();
+    if (lane == 0) atomicMax(&newest, top);
+    __syncthreads();
+    const int64_t but = (int64_t)newest - e.recent;
+    if constexpr (KEYS > 0) {  // (every lane's own slots, here and in every pass)
+#pragma unroll
+        for (int r = 0; r < kHeld; r++) {
+            const int32_t i = first + 64 * r;
+            if (r < rounds && i < n) keys[i] = evict_key(m[r], (int32_t)keys[i], but);
+        }
+    }
+    // f(slot, key, in) for every slot of this lane; in = false past the end, so that all lanes
+    // of a wavefront meet in its ballots.  Four keys are read together.
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        for (int32_t r = 0; r < rounds; r += 4) {
+            uint32_t k[4];
+            bool in[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int32_t i = first + 64 * (r + u);
+                in[u] = r + u < rounds && i < n;
+                k[u] = 0u;
+                if (in[u]) k[u] = KEYS ? keys[i] : evict_key(mass[i], pos[i], but);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; u++) f(first + 64 * (r + u), k[u], in[u]);
+        }
+    };
+
+    // the key of the last slot that is kept, by its leading 11, 11 and 10 bits
+    uint32_t prefix = 0, mask = 0;
+    int32_t left = keep;  // slots to keep among those with the prefix
+#pragma unroll
+    for (int pass = 0; pass < 3; pass++) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+        each([&](int32_t, uint32_t k, bool in) {
+            if (in && (k & mask) == prefix) atomicAdd(&hist[pass][(k >> shift) & (bins - 1)], 1u);
+        });
+        __syncthreads();
+        // from the top: this thread's two bins, and how many slots are in those above
+        const int32_t hi = bins - 1 - 2 * (int)threadIdx.x;
+        const int32_t h1 = hi > 0 ? (int32_t)hist[pass][hi] : 0;
+        const int32_t h0 = hi > 0 ? (int32_t)hist[pass][hi - 1] : 0;
+        int32_t run = wave_sums(h1 + h0);
+        if (lane == 63) sums[pass][wave] = run;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kEW; w++) {
+            const int32_t v = sums[pass][w];
+            run += w < wave ? v : 0;
+        }
+        const int32_t above = run - h1 - h0;
+        if (above < left && left <= run) {
+            const bool second = left > above + h1;
+            found[pass][0] = second ? hi - 1 : hi;
+            found[pass][1] = left - above - (second ? h1 : 0);
+        }
+        __syncthreads();
+        prefix |= (uint32_t)found[pass][0] << shift;
+        mask |= (uint32_t)(bins - 1) << shift;
+        left = found[pass][1];
+    }
+
+    // Slots below keep and at or above it whose key is larger, and ties (of which the first
+    // `left` are kept), in every wavefront's span; from these, what the spans before this one
+    // keep, free and move.
+    {
+        int4 v = {0, 0, 0, 0};
+        each([&](int32_t i, uint32_t k, bool in) {
+            const int32_t more = in && k > prefix, same = in && k == prefix;
+            if (i < keep) {
+                v.x += more;
+                v.y += same;
+            } else {
+                v.z += more;
+                v.w += same;
+            }
+        });
+        v = {wave_sums(v.x), wave_sums(v.y), wave_sums(v.z), wave_sums(v.w)};
+        if (lane == 63) counts[wave] = v;
+    }
+    __syncthreads();
+    int32_t ties = 0, some = 0, nf = 0, nm = 0, all = 0, t = 0;
+#pragma unroll
+    for (int w = 0; w < kEW; w++) {
+        const int4 v = counts[w];
+        const int32_t open = max(left - t, 0), low = min(v.y, open), high = min(v.w, open - low);
+        const int32_t slots_low = min(max(keep - w * rounds * 64, 0), rounds * 64);
+        if (w == wave) {
+            ties = t;
+            nf = all;
+            some = v.y + v.w;
+        }
+        if (w < wave) nm += v.z + high;
+        all += slots_low - v.x - low;
+        t += v.y + v.w;
+    }
+    if (threadIdx.x == 0) e.counts[blockIdx.x] = all;
+    const uint64_t below = (1ull << lane) - 1;
+    int32_t* freed = e.lists + (int64_t)blockIdx.x * 2 * e.moves;
+    each([&](int32_t i, uint32_t k, bool in) {
+        bool on = in && k > prefix;
+        if (some) {
+            const uint64_t tie = __ballot(in && k == prefix);
+            on |= in && k == prefix && ties + __popcll(tie & below) < left;
+            ties += __popcll(tie);
+        }
+        if (i - lane < keep) {  // (a wavefront's 64 slots: some below keep)
+            const uint64_t f = __ballot(in && i < keep && !on);
+            if (in && i < keep && !on) freed[nf + __popcll(f & below)] = i;
+            nf += __popcll(f);
+        }
+        if (i - lane + 63 >= keep) {
+            const uint64_t v = __ballot(i >= keep && on);
+            if (i >= keep && on) freed[e.moves + nm + __popcll(v & below)] = i;
+            nm += __popcll(v);
+        }
+    });
+}
+
+// The moves, 64 of a head to a workgroup: where each goes from and to, then the rows
+// (and their codebooks) in pieces of 16 bytes.
+constexpr int kMoves = 64, kVT = 256;
+
+__global__ __launch_bounds__(kVT) void k_kv_move(ecasq_kv_cache c, EvictPlan e, float* mass_out,
+                                                 int32_t* pos_out, int32_t* lens_out) {
+    __shared__ int64_t from[kMoves], to[kMoves];
+    const int32_t rows = c.batch * c.heads;
+    const int32_t row = blockIdx.x % rows, m0 = blockIdx.x / rows * kMoves;
+    const int32_t b = row / c.heads, head = row % c.heads;
+    if (m0 == 0 && head == 0 && threadIdx.x == 0) {  // (nothing else of this kernel reads lens)
+        const int64_t n = kv_len(c, b);
+        lens_out[b] = (int32_t)(n < e.keep ? n : e.keep);
+    }
+    const int32_t count = min(e.counts[row] - m0, kMoves);
+    if (count <= 0) return;
+    if ((int)threadIdx.x < count) {
+        const int32_t* freed = e.lists + (int64_t)row * 2 * e.moves + m0 + threadIdx.x;
+        const int32_t t = freed[0], f = freed[e.moves];
+        const int64_t base = (int64_t)row * kv_slots(c);
+        mass_out[base + t] = c.mass[base + f];
+        pos_out[base + t] = c.pos[base + f];
+        const int64_t rt = kv_row(c, b, head, t), rf = kv_row(c, b, head, f);
+        to[threadIdx.x] = rf < 0 ? -1 : rt;
+        from[threadIdx.x] = rf;
+    }
+    __syncthreads();
+    const int32_t piece = c.coded ? c.head_dim / 32 : c.head_dim / 8;  // of a row
+    const int32_t books = c.coded ? 2 : 0, each = 2 * (piece + books);
+    for (int32_t k = threadIdx.x; k < count * each; k += kVT) {
+        const int32_t m = k / each;
+        int32_t u = k % each;
+        if (to[m] < 0) continue;
+        const bool value = u >= piece + books;
+        if (value) u -= piece + books;
+        if (u < piece) {
+            uint4* x = static_cast<uint4*>(value ? c.v : c.k);
+            x[to[m] * piece + u] = x[from[m] * piece + u];
+        } else {
+            uint4* x = static_cast<uint4*>(value ? c.v_books : c.k_books);
+            x[to[m] * 2 + u - piece] = x[from[m] * 2 + u - piece];
+        }
     }
 }
 
-__global__ __launch_bounds__(256) void k_kv_lens(ecasq_kv_cache c, int32_t keep,
-                                                 int32_t* lens_out) {
-    const int32_t b = blockIdx.x * 256 + threadIdx.x;
-    if (b >= c.batch) return;
-    const int64_t n = kv_len(c, b);
-    lens_out[b] = (int32_t)(n < keep ? n : keep);
+EvictPlan evict_plan(const ecasq_kv_cache& c, int32_t keep, int32_t recent, char* ws) {
+    const int64_t slots = kv_slots(c);
+    EvictPlan e;
+    e.keep = (int32_t)(keep < slots ? keep : slots);
+    e.recent = recent;
+    e.moves = (int32_t)(slots - e.keep < e.keep ? slots - e.keep : e.keep);
+    e.counts = reinterpret_cast<int32_t*>(ws);
+    e.lists = e.counts + (int64_t)c.batch * c.heads;
+    return e;
 }
 
 }  // namespace
@@ -254,16 +405,24 @@ hipError_t launch_kv_write(const ecasq_kv_cache& c, const KvNew& n, hipStream_t 
 }
 
 size_t kv_evict_bytes(const ecasq_kv_cache& c, int32_t keep) {
-    const int64_t most = keep < kv_slots(c) ? keep : kv_slots(c);
-    return 256 + (size_t)c.batch * c.heads * 2 * most * sizeof(int32_t);
+    const EvictPlan e = evict_plan(c, keep, 0, nullptr);
+    return 256 + (size_t)c.batch * c.heads * (1 + 2 * (size_t)e.moves) * sizeof(int32_t);
 }
 
 hipError_t launch_kv_evict(const ecasq_kv_cache& c, int32_t keep, int32_t recent, float* mass_out,
                            int32_t* pos_out, int32_t* lens_out, char* ws, hipStream_t st) {
-    if (keep > kv_slots(c)) keep = (int32_t)kv_slots(c);
-    k_kv_evict<<<(unsigned)(c.batch * c.heads), kET, 0, st>>>(c, keep, recent, mass_out, pos_out,
-                                                              reinterpret_cast<int32_t*>(ws));
-    k_kv_lens<<<(unsigned)((c.batch + 255) / 256), 256, 0, st>>>(c, keep, lens_out);
+    const EvictPlan e = evict_plan(c, keep, recent, ws);
+    const unsigned rows = (unsigned)(c.batch * c.heads);
+    if (kv_slots(c) <= kKeysFew)
+        k_kv_evict<kKeysFew><<<rows, kET, 0, st>>>(c, e, mass_out, pos_out);
+    else if (kv_slots(c) <= kKeysMany)
+        k_kv_evict<kKeysMany><<<rows, kET, 0, st>>>(c, e, mass_out, pos_out);
+    else
+        k_kv_evict<0><<<rows, kET, 0, st>>>(c, e, mass_out, pos_out);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    const unsigned parts = (unsigned)(e.moves < 1 ? 1 : (e.moves + kMoves - 1) / kMoves);
+    k_kv_move<<<rows * parts, kVT, 0, st>>>(c, e, mass_out, pos_out, lens_out);
     return hipGetLastError();
 }
 
