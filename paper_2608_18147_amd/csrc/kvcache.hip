@@ -21,87 +21,156 @@ __device__ __forceinline__ int32_t sequence_of(const int32_t* __restrict__ start
     return n;
 }
 
-// A row's codebook in LDS, its values rounded to the cache's type beside them.
-struct RowBook {
-    double q[16];
-    int32_t t;
+// Where new row i goes, for a whole workgroup: its sequence, slot and page (-1: none), with
+// the slot's weight and position set; false if it is left out.
+struct Place {
+    int32_t b, page, offset;
 };
-
-// A workgroup per new token.
-template <int DT>
-__global__ __launch_bounds__(kWT) void k_kv_write(ecasq_kv_cache c, KvNew n) {
-    const int64_t i = blockIdx.x, slots = kv_slots(c);
-    const int32_t b = sequence_of(n.starts, c.batch, i);
-    if (b >= c.batch || n.starts[b] > i) return;
-    const int64_t slot = (int64_t)c.lens[b] - n.starts[b + 1] + i;
-    if (slot < 0 || slot >= slots) return;
+__device__ __forceinline__ bool place_of(const ecasq_kv_cache& c, const KvNew& n, int64_t i,
+                                         Place& p) {
+    const int64_t slots = kv_slots(c);
+    p.b = sequence_of(n.starts, c.batch, i);
+    if (p.b >= c.batch || n.starts[p.b] > i) return false;
+    const int64_t slot = (int64_t)c.lens[p.b] - n.starts[p.b + 1] + i;
+    if (slot < 0 || slot >= slots) return false;
     for (int32_t h = threadIdx.x; h < c.heads; h += kWT) {
-        const int64_t at = ((int64_t)b * c.heads + h) * slots + slot;
+        const int64_t at = ((int64_t)p.b * c.heads + h) * slots + slot;
         if (c.mass) c.mass[at] = 0.0f;
         if (c.pos) c.pos[at] = n.positions ? n.positions[i] : (int32_t)slot;
     }
-    const int32_t d = c.head_dim;
-    if (!c.coded) {
-        const int32_t chunks = d / 8;
-        for (int32_t e = threadIdx.x; e < 2 * c.heads * chunks; e += kWT) {
-            const bool value = e >= c.heads * chunks;
-            const int32_t r = value ? e - c.heads * chunks : e;
-            const int64_t row = kv_row(c, b, r / chunks, slot);
-            if (row < 0) return;
-            const auto* from = static_cast<const uint16_t*>(value ? n.v : n.k) +
-                               i * (value ? n.v_stride : n.k_stride) + (int64_t)r * 8;
-            uint4 v;
-            __builtin_memcpy(&v, from, 16);
-            reinterpret_cast<uint4*>(value ? c.v : c.k)[row * chunks + r % chunks] = v;
-        }
-        return;
+    p.page = c.table[(int64_t)p.b * c.max_pages + slot / c.page_size];
+    p.offset = (int32_t)(slot % c.page_size);
+    return p.page >= 0 && p.page < c.n_pages;
+}
+
+// Rows of 16-bit values: a workgroup per token, 16 bytes a thread.
+__global__ __launch_bounds__(kWT) void k_kv_write(ecasq_kv_cache c, KvNew n) {
+    const int64_t i = blockIdx.x;
+    Place p;
+    if (!place_of(c, n, i, p)) return;
+    const int32_t chunks = c.head_dim / 8;
+    for (int32_t e = threadIdx.x; e < 2 * c.heads * chunks; e += kWT) {
+        const bool value = e >= c.heads * chunks;
+        const int32_t r = value ? e - c.heads * chunks : e;
+        const int64_t row = ((int64_t)p.page * c.heads + r / chunks) * c.page_size + p.offset;
+        const auto* from = static_cast<const uint16_t*>(value ? n.v : n.k) +
+                           i * (value ? n.v_stride : n.k_stride) + (int64_t)r * 8;
+        uint4 v;
+        __builtin_memcpy(&v, from, 16);
+        reinterpret_cast<uint4*>(value ? c.v : c.k)[row * chunks + r % chunks] = v;
     }
-    __shared__ RowBook books[kWT / 32];
-    const int32_t lanes = d / 2, per = kWT / lanes;  // a thread per pair of entries
-    const int32_t mine = threadIdx.x / lanes, pair = threadIdx.x % lanes;
+}
+
+// A row's codebook in a wavefront's LDS: the values; the largest floats not above the
+// values 1 .. t - 2, and infinity (a float x is above value k exactly if it is above that
+// float); about one over the intervals' widths (NaN where that is no ordinary float); the
+// values in the cache's type.
+struct RowBook {
+    double q[16];
+    float s[16], over[16];
+    uint16_t h[16];
+    int32_t t;
+};
+
+__device__ __forceinline__ float float_not_above(double q) {
+    const float f = (float)q;
+    if (!((double)f > q)) return f;
+    const uint32_t b = __float_as_uint(f);
+    return __uint_as_float((b & 0x7FFFFFFFu) == 0u ? 0x80000001u : (b >> 31) ? b + 1u : b - 1u);
+}
+
+// Rows of symbols: a workgroup per token, a wavefront per 128 entries (a row, two or half
+// of one), two entries a lane from one call of the generator.  Brackets and comparisons are
+// made in 32 bits where those decide, as in ecasq_quantize: the quotient in 32 bits is within
+// 2^-21 of the one in 64 up to 2, and the uniform within 2^-24, so that only a difference
+// below 2^-20 (one entry in 2^19, or NaN) takes the 64-bit division.  The generator's 20
+// products are the larger part of the instructions (4000 tokens of 8 heads of 128: 52 us with
+// 64-bit comparisons, FIXME us so).
+template <int DT, int D>
+__global__ __launch_bounds__(kWT) void k_kv_round(ecasq_kv_cache c, KvNew n) {
+    constexpr int kRows = D < 128 ? 128 / D : 1, kParts = D < 128 ? 1 : D / 128;
+    __shared__ RowBook lds[kWT / 64][kRows];
+    const int64_t i = blockIdx.x;
+    Place p;
+    if (!place_of(c, n, i, p)) return;
+    const int lane = threadIdx.x % 64;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t k0 = (uint32_t)n.seed, k1 = (uint32_t)(n.seed >> 32);
-    for (int32_t r0 = 0; r0 < 2 * c.heads; r0 += per) {
-        const int32_t r = r0 + mine;
-        const bool live = r < 2 * c.heads, value = r >= c.heads;
-        const int32_t head = value ? r - c.heads : r;
-        const int64_t row = live ? kv_row(c, b, head, slot) : -1, in = i * c.heads + head;
-        __syncthreads();
-        if (row >= 0 && pair < 16) {
-            const int32_t t = (value ? n.v_counts : n.k_counts)[in];
+    const int32_t units = (c.heads + kRows - 1) / kRows * kParts;  // of keys, and of values
+    RowBook* books = lds[wave];
+    for (int32_t u = wave; u < 2 * units; u += kWT / 64) {
+        const bool value = u >= units;
+        const int32_t v = value ? u - units : u, part = v % kParts, head0 = v / kParts * kRows;
+        const int64_t row0 = ((int64_t)p.page * c.heads + head0) * c.page_size + p.offset;
+        const int64_t in0 = i * c.heads + head0;
+        // the books: a lane per value
+        {
+            const int r = lane / 16, k = lane % 16;
+            const bool live = r < kRows && head0 + r < c.heads;
+            int32_t t = 0;
+            if (live) t = (value ? n.v_counts : n.k_counts)[in0 + r];
             const bool good = t >= 1 && t <= 16 && t <= n.s;
-            const double q =
-                good && pair < t ? (value ? n.v_books : n.k_books)[in * n.s + pair] : 0.0;
-            books[mine].q[pair] = q;
-            if (pair == 0) books[mine].t = good ? t : 0;
-            static_cast<uint16_t*>(value ? c.v_books : c.k_books)[row * 16 + pair] =
-                good ? to16<DT>(q) : kNan16<DT>;
+            t = good ? t : 0;
+            double q = 0.0;
+            if (k < t) q = (value ? n.v_books : n.k_books)[(in0 + r) * n.s + k];
+            const double width = __shfl_down(q, 1) - q;
+            const uint16_t h = good ? to16<DT>(q) : kNan16<DT>;
+            __builtin_amdgcn_wave_barrier();  // the last unit's reads come first
+            if (live) {
+                RowBook& B = books[r];
+                B.q[k] = q;
+                B.s[k] = k >= 1 && k <= t - 2 ? float_not_above(q) : __builtin_huge_valf();
+                B.over[k] = k < t - 1 && width >= 0x1p-100 && width <= 0x1p+100
+                                ? 1.0f / (float)width
+                                : __builtin_nanf("");
+                B.h[k] = h;
+                if (k == 0) B.t = t;
+                if (part == 0)
+                    static_cast<uint16_t*>(value ? c.v_books
+                                                 : c.k_books)[(row0 + (int64_t)r * c.page_size) * 16 +
+                                                              k] = h;
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-        __syncthreads();
-        if (row < 0) continue;
-        const RowBook& B = books[mine];
+        const int r = kRows > 1 ? lane / (D / 2) : 0;
+        const int pair = kRows > 1 ? lane % (D / 2) : part * 64 + lane;
+        if (head0 + r >= c.heads) continue;
+        const RowBook& B = books[r];
+        const int64_t in = in0 + r, row = row0 + (int64_t)r * c.page_size;
         uint32_t sym[2] = {0u, 0u};
         if (B.t > 1) {
-            const int64_t h = (in * d) / 2 + pair;
+            uint32_t two;
+            __builtin_memcpy(&two,
+                             static_cast<const uint16_t*>(value ? n.v : n.k) +
+                                 i * (value ? n.v_stride : n.k_stride) +
+                                 (int64_t)(head0 + r) * D + 2 * pair,
+                             4);
+            const float x[2] = {from16<DT>(two & 0xFFFFu), from16<DT>(two >> 16)};
+            uint32_t at[2] = {0u, 0u};
+#pragma unroll
+            for (uint32_t step = 8; step > 0; step /= 2)
+#pragma unroll
+                for (int e = 0; e < 2; e++)
+                    if (B.s[at[e] + step] < x[e]) at[e] += step;
+            const int64_t h = (in * D) / 2 + pair;
             uint32_t w[4] = {(uint32_t)h, (uint32_t)(h >> 32), value ? 3u : 2u, 0u};
             philox4x32_10(w, k0, k1);
-            const auto* from = static_cast<const uint16_t*>(value ? n.v : n.k) +
-                               i * (value ? n.v_stride : n.k_stride) + (int64_t)head * d + 2 * pair;
 #pragma unroll
             for (int e = 0; e < 2; e++) {
-                const double x = (double)from16<DT>(from[e]);
-                int32_t at = 0;
-                for (int32_t k = 1; k <= B.t - 2; k++)
-                    if (B.q[k] < x) at = k;
-                const double p = (x - B.q[at]) / (B.q[at + 1] - B.q[at]);
-                sym[e] = at + (uniform53(w[2 * e], w[2 * e + 1]) < p ? 1 : 0);
+                const double a = B.q[at[e]], N = (double)x[e] - a;
+                const float d = (float)w[2 * e + 1] * 0x1p-32f - (float)N * B.over[at[e]];
+                bool up = d < 0.0f;
+                if (!(__builtin_fabsf(d) > 0x1p-20f))
+                    up = uniform53(w[2 * e], w[2 * e + 1]) < N / (B.q[at[e] + 1] - a);
+                sym[e] = at[e] + (up ? 1u : 0u);
             }
         }
-        static_cast<uint8_t*>(value ? c.v : c.k)[row * lanes + pair] =
+        static_cast<uint8_t*>(value ? c.v : c.k)[row * (D / 2) + pair] =
             (uint8_t)(sym[0] | (sym[1] << 4));
         if (n.k_hat) {
-            auto* to = static_cast<uint16_t*>(value ? n.v_hat : n.k_hat) + in * d + 2 * pair;
-#pragma unroll
-            for (int e = 0; e < 2; e++) to[e] = B.t ? to16<DT>(B.q[sym[e]]) : kNan16<DT>;
+            const uint32_t two = B.h[sym[0]] | (uint32_t)B.h[sym[1]] << 16;
+            __builtin_memcpy(static_cast<uint16_t*>(value ? n.v_hat : n.k_hat) + in * D + 2 * pair,
+                             &two, 4);
         }
     }
 }
@@ -135,8 +204,9 @@ __device__ __forceinline__ int32_t wave_sums(int32_t v) {
 // slots, 64 at a time, so that ranks in slot order are a ballot's and three barriers'
 // work.  The keys are in LDS (KEYS of them; in registers, 32 to a thread, the unrolled
 // passes took 17 us for the shortest heads); longer heads (KEYS = 0) read mass and pos
-// again for every pass.  What is bounded by one CU's instructions for a long head is
-// bounded by the passes' latencies for a short one (FIXME).
+// again for every pass.  A long head is bounded by what one CU reads
+// and issues (32768 slots: 44 us, 13 of them until mass and pos are there), a short one by
+// the passes' latencies (640 slots: 8 us).
 constexpr int kEW = kET / 64, kBins = 2048;
 constexpr int kKeysFew = 4096, kKeysMany = 32768;
 
@@ -396,11 +466,27 @@ EvictPlan evict_plan(const ecasq_kv_cache& c, int32_t keep, int32_t recent, char
 
 }  // namespace
 
-hipError_t launch_kv_write(const ecasq_kv_cache& c, const KvNew& n, hipStream_t st) {
-    if (c.dt == ECASQ_F16)
-        k_kv_write<1><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+namespace {
+
+template <int DT>
+void kv_round(const ecasq_kv_cache& c, const KvNew& n, hipStream_t st) {
+    if (c.head_dim == 64)
+        k_kv_round<DT, 64><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+    else if (c.head_dim == 128)
+        k_kv_round<DT, 128><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
     else
-        k_kv_write<2><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+        k_kv_round<DT, 256><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+}
+
+}  // namespace
+
+hipError_t launch_kv_write(const ecasq_kv_cache& c, const KvNew& n, hipStream_t st) {
+    if (!c.coded)
+        k_kv_write<<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+    else if (c.dt == ECASQ_F16)
+        kv_round<1>(c, n, st);
+    else
+        kv_round<2>(c, n, st);
     return hipGetLastError();
 }
 
