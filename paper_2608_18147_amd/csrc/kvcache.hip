@@ -33,13 +33,14 @@ __device__ __forceinline__ bool place_of(const ecasq_kv_cache& c, const KvNew& n
     if (p.b >= c.batch || n.starts[p.b] > i) return false;
     const int64_t slot = (int64_t)c.lens[p.b] - n.starts[p.b + 1] + i;
     if (slot < 0 || slot >= slots) return false;
-    for (int32_t h = threadIdx.x; h < c.heads; h += kWT) {
+    for (int32_t h = threadIdx.x; blockIdx.y == 0 && h < c.heads; h += kWT) {
         const int64_t at = ((int64_t)p.b * c.heads + h) * slots + slot;
         if (c.mass) c.mass[at] = 0.0f;
         if (c.pos) c.pos[at] = n.positions ? n.positions[i] : (int32_t)slot;
     }
-    p.page = c.table[(int64_t)p.b * c.max_pages + slot / c.page_size];
-    p.offset = (int32_t)(slot % c.page_size);
+    const uint32_t at = (uint32_t)slot, size = (uint32_t)c.page_size;  // below 2^30
+    p.page = c.table[(int64_t)p.b * c.max_pages + at / size];
+    p.offset = (int32_t)(at % size);
     return p.page >= 0 && p.page < c.n_pages;
 }
 
@@ -84,35 +85,70 @@ __device__ __forceinline__ float float_not_above(double q) {
 // made in 32 bits where those decide, as in ecasq_quantize: the quotient in 32 bits is within
 // 2^-21 of the one in 64 up to 2, and the uniform within 2^-24, so that only a difference
 // below 2^-20 (one entry in 2^19, or NaN) takes the 64-bit division.  The generator's 20
-// products are the larger part of the instructions (4000 tokens of 8 heads of 128: 52 us with
-// 64-bit comparisons, FIXME us so).
+// products are the larger part of the instructions (4000 tokens of 8 heads of 128: 50 us with
+// 64-bit comparisons, 30 so).
 template <int DT, int D>
 __global__ __launch_bounds__(kWT) void k_kv_round(ecasq_kv_cache c, KvNew n) {
     constexpr int kRows = D < 128 ? 128 / D : 1, kParts = D < 128 ? 1 : D / 128;
     __shared__ RowBook lds[kWT / 64][kRows];
     const int64_t i = blockIdx.x;
-    Place p;
-    if (!place_of(c, n, i, p)) return;
-    const int lane = threadIdx.x % 64;
+    const int lane = threadIdx.x % 64, r = lane / 16, k = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int mine = kRows > 1 ? lane / (D / 2) : 0;
     const uint32_t k0 = (uint32_t)n.seed, k1 = (uint32_t)(n.seed >> 32);
     const int32_t units = (c.heads + kRows - 1) / kRows * kParts;  // of keys, and of values
+    const int32_t last = min(2 * units, (int32_t)(blockIdx.y + 1) * n.units);
     RowBook* books = lds[wave];
-    for (int32_t u = wave; u < 2 * units; u += kWT / 64) {
-        const bool value = u >= units;
-        const int32_t v = value ? u - units : u, part = v % kParts, head0 = v / kParts * kRows;
+    // what a unit reads, on the way while the one before is rounded (and, the first, while
+    // the row's place is found): a lane's count and value of the books, and two entries
+    struct Unit {
+        bool value;
+        int32_t part, head0, t, pair;
+        uint32_t two;
+        double q;
+    };
+    auto read = [&](int32_t u) {
+        Unit x;
+        x.value = u >= units;
+        const int32_t v = x.value ? u - units : u;
+        x.part = v % kParts;
+        x.head0 = v / kParts * kRows;
+        x.pair = kRows > 1 ? lane % (D / 2) : x.part * 64 + lane;
+        x.t = 0;
+        x.two = 0u;
+        x.q = 0.0;
+        if (u >= last) return x;
+        const int64_t in0 = i * c.heads + x.head0;
+        if (x.head0 + mine < c.heads)
+            __builtin_memcpy(&x.two,
+                             static_cast<const uint16_t*>(x.value ? n.v : n.k) +
+                                 i * (x.value ? n.v_stride : n.k_stride) +
+                                 (int64_t)(x.head0 + mine) * D + 2 * x.pair,
+                             4);
+        if (r < kRows && x.head0 + r < c.heads) {
+            x.t = (x.value ? n.v_counts : n.k_counts)[in0 + r];
+            if (k < n.s) x.q = (x.value ? n.v_books : n.k_books)[(in0 + r) * n.s + k];
+        }
+        return x;
+    };
+    int32_t u = (int32_t)blockIdx.y * n.units + wave;
+    Unit next = read(u);
+    Place p;
+    if (!place_of(c, n, i, p)) return;
+    for (; u < last; u += kWT / 64) {
+        const Unit now = next;
+        next = read(u + kWT / 64);
+        const bool value = now.value;
+        const int32_t head0 = now.head0, part = now.part, pair = now.pair;
+        const uint32_t two = now.two;
         const int64_t row0 = ((int64_t)p.page * c.heads + head0) * c.page_size + p.offset;
         const int64_t in0 = i * c.heads + head0;
         // the books: a lane per value
         {
-            const int r = lane / 16, k = lane % 16;
             const bool live = r < kRows && head0 + r < c.heads;
-            int32_t t = 0;
-            if (live) t = (value ? n.v_counts : n.k_counts)[in0 + r];
-            const bool good = t >= 1 && t <= 16 && t <= n.s;
-            t = good ? t : 0;
-            double q = 0.0;
-            if (k < t) q = (value ? n.v_books : n.k_books)[(in0 + r) * n.s + k];
+            const bool good = now.t >= 1 && now.t <= 16 && now.t <= n.s;
+            const int32_t t = good ? now.t : 0;
+            const double q = k < t ? now.q : 0.0;
             const double width = __shfl_down(q, 1) - q;
             const uint16_t h = good ? to16<DT>(q) : kNan16<DT>;
             __builtin_amdgcn_wave_barrier();  // the last unit's reads come first
@@ -132,19 +168,11 @@ __global__ __launch_bounds__(kWT) void k_kv_round(ecasq_kv_cache c, KvNew n) {
             }
             __builtin_amdgcn_wave_barrier();
         }
-        const int r = kRows > 1 ? lane / (D / 2) : 0;
-        const int pair = kRows > 1 ? lane % (D / 2) : part * 64 + lane;
-        if (head0 + r >= c.heads) continue;
-        const RowBook& B = books[r];
-        const int64_t in = in0 + r, row = row0 + (int64_t)r * c.page_size;
+        if (head0 + mine >= c.heads) continue;
+        const RowBook& B = books[mine];
+        const int64_t in = in0 + mine, row = row0 + (int64_t)mine * c.page_size;
         uint32_t sym[2] = {0u, 0u};
         if (B.t > 1) {
-            uint32_t two;
-            __builtin_memcpy(&two,
-                             static_cast<const uint16_t*>(value ? n.v : n.k) +
-                                 i * (value ? n.v_stride : n.k_stride) +
-                                 (int64_t)(head0 + r) * D + 2 * pair,
-                             4);
             const float x[2] = {from16<DT>(two & 0xFFFFu), from16<DT>(two >> 16)};
             uint32_t at[2] = {0u, 0u};
 #pragma unroll
@@ -168,9 +196,9 @@ __global__ __launch_bounds__(kWT) void k_kv_round(ecasq_kv_cache c, KvNew n) {
         static_cast<uint8_t*>(value ? c.v : c.k)[row * (D / 2) + pair] =
             (uint8_t)(sym[0] | (sym[1] << 4));
         if (n.k_hat) {
-            const uint32_t two = B.h[sym[0]] | (uint32_t)B.h[sym[1]] << 16;
+            const uint32_t hat = B.h[sym[0]] | (uint32_t)B.h[sym[1]] << 16;
             __builtin_memcpy(static_cast<uint16_t*>(value ? n.v_hat : n.k_hat) + in * D + 2 * pair,
-                             &two, 4);
+                             &hat, 4);
         }
     }
 }
@@ -468,14 +496,26 @@ EvictPlan evict_plan(const ecasq_kv_cache& c, int32_t keep, int32_t recent, char
 
 namespace {
 
+template <int DT, int D>
+void kv_round(const ecasq_kv_cache& c, KvNew n, hipStream_t st) {
+    // Units of 128 entries: four for each wavefront of a workgroup, or fewer while there are
+    // not four workgroups to a CU (152 tokens of 8 heads of 256: 6.9 us with four, 5.0 with two;
+    // 4000 of 8 of 128: 30 and 32).
+    const int64_t units = 2 * (((int64_t)c.heads * D + 127) / 128);
+    n.units = 4 * kWT / 64;
+    while (n.units > kWT / 64 && n.rows * ((units + n.units - 1) / n.units) < 1024) n.units /= 2;
+    const dim3 g((unsigned)n.rows, (unsigned)((units + n.units - 1) / n.units));
+    k_kv_round<DT, D><<<g, kWT, 0, st>>>(c, n);
+}
+
 template <int DT>
 void kv_round(const ecasq_kv_cache& c, const KvNew& n, hipStream_t st) {
     if (c.head_dim == 64)
-        k_kv_round<DT, 64><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+        kv_round<DT, 64>(c, n, st);
     else if (c.head_dim == 128)
-        k_kv_round<DT, 128><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+        kv_round<DT, 128>(c, n, st);
     else
-        k_kv_round<DT, 256><<<(unsigned)n.rows, kWT, 0, st>>>(c, n);
+        kv_round<DT, 256>(c, n, st);
 }
 
 }  // namespace

@@ -90,7 +90,14 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache* c, const void* new_k, int64_t 
     const int64_t row = (int64_t)c->heads * c->head_dim, most = (int64_t)1 << 30;
     if (k_stride < row || v_stride < row || k_stride > most || v_stride > most)
         return ECASQ_EINVAL;
-    KvNew n{new_k, new_v, k_stride, v_stride, rows, starts, positions};
+    KvNew n{};
+    n.k = new_k;
+    n.v = new_v;
+    n.k_stride = k_stride;
+    n.v_stride = v_stride;
+    n.rows = rows;
+    n.starts = starts;
+    n.positions = positions;
     if (c->coded) {
         if (!k_codebooks || !k_counts || !v_codebooks || !v_counts || s < 2 || s > 32 ||
             (k_hat == nullptr) != (v_hat == nullptr) || !aligned(k_hat, 2) || !aligned(v_hat, 2))

@@ -34,10 +34,11 @@ hipError_t launch_matvec(const char* packed, int dt, const Weights& w, const voi
 // ---- kvcache.hip ----
 // Where a slot's rows are: an index of rows of the cache, or -1.
 __device__ __forceinline__ int64_t kv_row(const ecasq_kv_cache& c, int32_t b, int32_t head,
-                                          int64_t slot) {
-    const int32_t page = c.table[(int64_t)b * c.max_pages + slot / c.page_size];
+                                          int32_t slot) {
+    const uint32_t at = (uint32_t)slot, size = (uint32_t)c.page_size;
+    const int32_t page = c.table[(int64_t)b * c.max_pages + at / size];
     if (page < 0 || page >= c.n_pages) return -1;
-    return ((int64_t)page * c.heads + head) * c.page_size + slot % c.page_size;
+    return ((int64_t)page * c.heads + head) * c.page_size + at % size;
 }
 __host__ __device__ __forceinline__ int64_t kv_slots(const ecasq_kv_cache& c) {
     return (int64_t)c.max_pages * c.page_size;
@@ -55,6 +56,7 @@ struct KvNew {
     int32_t s;
     uint64_t seed;
     void *k_hat, *v_hat;
+    int32_t units;  // of a workgroup (set by the launch)
 };
 hipError_t launch_kv_write(const ecasq_kv_cache& c, const KvNew& n, hipStream_t st);
 size_t kv_evict_bytes(const ecasq_kv_cache& c, int32_t keep);
