@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache
                                                 float2* __restrict__ ml, float* __restrict__ part) {
     constexpr int J = D / 32;   // products per tile of S'
     constexpr int E = D / 16;   // entries of a value row per lane
-    constexpr int MERGE = 2 * 64 * (D / 4 + 2) * 4;
+    constexpr int MERGE = kWaves * (64 * D + 128);  // a wavefront's O', m and l
     constexpr int LDS = CODED && kWaves * kBookBytes > MERGE ? kWaves * kBookBytes : MERGE;
     __shared__ __align__(256) uint8_t lds[LDS];
 
@@ -369,57 +369,56 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache
         }
     }
 
-    // the sum over the head's four lanes, then the wavefronts, two and two
+    // The wavefronts' parts meet in LDS: O' as [E][head][g] of four entries, so that 16 threads
+    // a head read them in order, then m and l (summed over the head's four lanes).
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    __syncthreads();
+    if (mine) {
+        float* to = reinterpret_cast<float*>(lds) + wave * (16 * D + 32);
 #pragma unroll
-    for (int half = kWaves / 2; half > 0; half /= 2) {
-        __syncthreads();
-        float* to = reinterpret_cast<float*>(lds);
-        if (wave >= half && wave < 2 * half) {
-            float* x = to + (wave - half) * 64 * (D / 4 + 2);
-            x[lane] = m;
-            x[64 + lane] = l;
-#pragma unroll
-            for (int i = 0; i < E; i++)
-                *reinterpret_cast<f32x4*>(x + 128 + i * 256 + 4 * lane) = acc[i];
-        }
-        __syncthreads();
-        if (wave < half) {
-            const float* x = to + wave * 64 * (D / 4 + 2);
-            const float m2 = x[lane], M = fmaxf(m, m2);
-            const float d1 = down_to(m, M), d2 = down_to(m2, M);
-            m = M;
-            l = l * d1 + x[64 + lane] * d2;
-#pragma unroll
-            for (int i = 0; i < E; i++)
-                acc[i] = acc[i] * d1 +
-                         *reinterpret_cast<const f32x4*>(x + 128 + i * 256 + 4 * lane) * d2;
+        for (int i = 0; i < E; i++)
+            *reinterpret_cast<f32x4*>(to + i * 256 + (n16 * 4 + g) * 4) = acc[i];
+        if (g == 0) {
+            to[16 * D + n16] = m;
+            to[16 * D + 16 + n16] = l;
         }
     }
-    if (wave != 0 || !mine) return;
-    // entries (4 g + r) E + i of the lane's head
-    const bool whole = used <= 1;
-    if (ml && g == 0) ml[row_out * p.chunks + ch] = make_float2(m, l);
-    const float by = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+    __syncthreads();
+    // entries (4 g + r) E + i of head o16, by thread 16 o16 + 4 g + r
+    static_assert(kAT == 256, "16 heads by 16 threads");
+    const int o16 = threadIdx.x / 16, quad = threadIdx.x % 16;
+    if (ht * 16 + o16 >= p.group) return;
+    const float* from = reinterpret_cast<const float*>(lds);
+    constexpr int kPart = 16 * D + 32;
+    float M = -INFINITY, L = 0.0f, down[kWaves], o[E];
 #pragma unroll
-    for (int r = 0; r < 4; r++) {
-        float o[E];
+    for (int w = 0; w < kWaves; w++) M = fmaxf(M, from[w * kPart + 16 * D + o16]);
 #pragma unroll
-        for (int i = 0; i < E; i++) o[i] = acc[i][r] * by;
-        if (whole) {
-            uint32_t w[E / 2];
-#pragma unroll
-            for (int i = 0; i < E / 2; i++)
-                w[i] = to16<DT>(o[2 * i]) | (uint32_t)to16<DT>(o[2 * i + 1]) << 16;
-            __builtin_memcpy(__builtin_assume_aligned(out + row_out * D + (4 * g + r) * E, 8), w,
-                             2 * E);
-        } else {
-            __builtin_memcpy(__builtin_assume_aligned(
-                                 part + (row_out * p.chunks + ch) * D + (4 * g + r) * E, 16),
-                             o, 4 * E);
-        }
+    for (int w = 0; w < kWaves; w++) {
+        down[w] = down_to(from[w * kPart + 16 * D + o16], M);
+        L += from[w * kPart + 16 * D + 16 + o16] * down[w];
     }
+#pragma unroll
+    for (int i = 0; i < E; i++) {
+        o[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++)
+            o[i] += from[w * kPart + i * 256 + threadIdx.x] * down[w];
+    }
+    const int64_t row = ((int64_t)b * c.heads + head) * p.group + ht * 16 + o16;
+    if (ml && quad == 0) ml[row * p.chunks + ch] = make_float2(M, L);
+    if (used > 1) {
+        __builtin_memcpy(
+            __builtin_assume_aligned(part + (row * p.chunks + ch) * D + quad * E, 16), o, 4 * E);
+        return;
+    }
+    const float by = L == 0.0f ? 0.0f : 1.0f / L;
+    uint32_t w[E / 2];
+#pragma unroll
+    for (int i = 0; i < E / 2; i++)
+        w[i] = to16<DT>(o[2 * i] * by) | (uint32_t)to16<DT>(o[2 * i + 1] * by) << 16;
+    __builtin_memcpy(__builtin_assume_aligned(out + row * D + quad * E, 8), w, 2 * E);
 }
 
 // Joins the chunks of every sequence that has more than one, a workgroup per query
