@@ -418,7 +418,7 @@ ecasq_status ecasq_matvec(const void *packed, ecasq_dtype dt, int64_t n_out, int
  *     (ecasq_solve_batched): 4 + 256 / head_dim bits an entry.
  * dt is ECASQ_F16 or ECASQ_BF16; head_dim 64, 128 or 256; page_size a multiple
  * of 16, 16 to 65536, and max_pages page_size at most 2^30; 1 <= heads <= 1024;
- * 1 <= batch <= 65535; k, v and the books are 16-byte aligned.  lens[b] is the number of slots of sequence b in
+ * 1 <= batch <= 65535, batch heads at most 2^20; k, v and the books are 16-byte aligned.  lens[b] is the number of slots of sequence b in
  * use; a number below 0 counts as 0, one above max_pages page_size as that.  The
  * slots of a table entry outside [0, n_pages) hold nothing: they are not read,
  * not written, and get no weight.  A page with slots that a call writes must
@@ -452,7 +452,7 @@ typedef struct {
  * starts[b] .. starts[b+1]-1 are sequence b's new tokens, and lens already counts
  * them: row i goes to slot lens[b] - starts[b+1] + i (advance lens first; a
  * slot below 0 or past the table, or a row that no sequence has, is left out).
- * new_k, new_v: device, `rows` tokens of heads x head_dim entries of dt, k_stride
+ * new_k, new_v: device, `rows` (1 to 2^23) tokens of heads x head_dim entries of dt, k_stride
  * and v_stride (>= heads head_dim) entries apart, of their type's alignment.
  * With c->mass, the slot's weight becomes 0; with c->pos, its position becomes
  * positions[i], or the slot itself where positions is NULL.
@@ -484,14 +484,15 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  *   scale q[b][h] . K[b][g][t],  g = h heads / q_heads;
  * q: device, batch rows of q_heads x head_dim entries of dt, q_stride >= q_heads
  * head_dim entries apart, of their type's alignment; q_heads a multiple of heads,
- * at most 64 heads, and batch q_heads at most 2^28; out: device, batch x q_heads x head_dim of dt, 16-byte
+ * at most 64 heads, and batch q_heads at most 2^23; out: device, batch x q_heads x head_dim of dt, 16-byte
  * aligned.  Scores, weights and sums are fp32; out is rounded once.  A sequence
  * with no slots to read, or whose scores are all -inf, gives zeros.  A NaN or
  * infinity in a row that is read reaches the result; what lies in slots past
  * lens[b] does not.
  * mass_out (device, as c->mass; NULL: no weights): for each slot below lens[b]
  * and head g, c->mass (0 where that is NULL) plus p_t summed over g's query heads
- * in order; slots past lens[b] are left as they are.  mass_out may be c->mass.
+ * in order; slots past lens[b] are left as they are.  mass_out may be c->mass; with it
+ * batch heads max_pages page_size is at most 2^30.
  * The length is split over workgroups and joined where batch and heads alone do
  * not fill the card; results are the same bit for bit from run to run.
  * workspace: at least ecasq_kv_attention_workspace bytes (0 for a bad cache or
@@ -513,7 +514,8 @@ ecasq_status ecasq_kv_attention(const ecasq_kv_cache *c, const void *q, int64_t 
  * are, and slots at or above keep may be given to another sequence after the
  * call.  mass_out, pos_out (as c->mass and c->pos, which are needed) receive the
  * slots below min(lens[b], keep), lens_out (batch) that number; they may be
- * c->mass, c->pos and c->lens.  keep >= 1, 0 <= recent <= keep.  Slots without
+ * c->mass, c->pos and c->lens.  keep >= 1, 0 <= recent <= keep, and batch heads max_pages
+ * page_size at most 2^30.  Slots without
  * a page are ranked and moved like others but have no rows (a row moved from one
  * leaves the freed slot's row as it was).
  * workspace: ecasq_kv_evict_workspace bytes (0 for a bad cache or keep), 256-byte

@@ -26,12 +26,15 @@ __global__ __launch_bounds__(256) void k_weights_pack(const uint8_t* __restrict_
             const int64_t block = at / 256;
             const int64_t o = block / w.blocks() * 16 + l % 16;
             const int64_t i0 = block % w.blocks() * 128 + 32 * j + 8 * (l / 16);
+            uint8_t eight[8];
+            const bool whole = o < w.n_out && i0 + 8 <= w.n_in;
+            if (whole) __builtin_memcpy(eight, sym + o * w.n_in + i0, 8);
             uint32_t v = 0;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 uint32_t s = pad;
                 if (o < w.n_out && i0 + i < w.n_in) {
-                    s = sym[o * w.n_in + i0 + i];
+                    s = whole ? eight[i] : sym[o * w.n_in + i0 + i];
                     s = s < (uint32_t)t ? s : (uint32_t)t - 1u;
                 }
                 v |= s << (4 * i);
@@ -357,12 +360,9 @@ hipError_t launch_matvec(const char* packed, int dt, const Weights& w, const voi
                          int64_t x_stride, void* y, hipStream_t st) {
     MatvecArgs a{};
     a.packed = packed;
-    a.x = static_cast<const uint16_t*>(x);
-    a.y = static_cast<uint16_t*>(y);
     a.x_stride = x_stride;
     a.n_out = w.n_out;
     a.n_in = (int32_t)w.n_in;
-    a.m = (int32_t)m;
     a.tiles = (int32_t)w.tiles();
     a.blocks = (int32_t)w.blocks();
     a.groups = (int32_t)w.groups();
@@ -396,20 +396,29 @@ hipError_t launch_matvec(const char* packed, int dt, const Weights& w, const voi
     a.turns = !many || in_lds ? 1 : a.slots < kTurns ? a.slots : kTurns;
     if (a.slots > kMW / a.parts) a.slots = kMW / a.parts;
     const int32_t each = a.slots * a.turns, wgs = (a.tiles + each - 1) / each;
-    const dim3 g((unsigned)(wgs < cus ? wgs : cus), (unsigned)((m + 15) / 16));
-    if (in_lds)
-        matvec_go<4, kManyLds>(a, dt, step, g, st);
-    else if (many)
-        matvec_go<4, kMany>(a, dt, step, g, st);
-    else if (nb == 1)
-        matvec_go<1, kOne>(a, dt, step, g, st);
-    else if (nb == 2)
-        matvec_go<2, kOne>(a, dt, step, g, st);
-    else if (nb == 3)
-        matvec_go<3, kOne>(a, dt, step, g, st);
-    else
-        matvec_go<4, kOne>(a, dt, step, g, st);
-    return hipGetLastError();
+    constexpr int64_t most = (int64_t)1 << 19;  // rows of one launch (its grid's second side)
+    for (int64_t r0 = 0; r0 < m; r0 += most) {
+        const int64_t rows = m - r0 < most ? m - r0 : most;
+        a.x = static_cast<const uint16_t*>(x) + r0 * x_stride;
+        a.y = static_cast<uint16_t*>(y) + r0 * w.n_out;
+        a.m = (int32_t)rows;
+        const dim3 g((unsigned)(wgs < cus ? wgs : cus), (unsigned)((rows + 15) / 16));
+        if (in_lds)
+            matvec_go<4, kManyLds>(a, dt, step, g, st);
+        else if (many)
+            matvec_go<4, kMany>(a, dt, step, g, st);
+        else if (nb == 1)
+            matvec_go<1, kOne>(a, dt, step, g, st);
+        else if (nb == 2)
+            matvec_go<2, kOne>(a, dt, step, g, st);
+        else if (nb == 3)
+            matvec_go<3, kOne>(a, dt, step, g, st);
+        else
+            matvec_go<4, kOne>(a, dt, step, g, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace ecasq

@@ -27,7 +27,8 @@ bool kv_sizes_ok(const ecasq_kv_cache* c) {
     return c && half_type(c->dt) && (c->coded == 0 || c->coded == 1) && c->heads >= 1 &&
            c->heads <= 1024 && (c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256) &&
            c->page_size >= 16 && c->page_size <= 65536 && c->page_size % 16 == 0 &&
-           c->batch >= 1 && c->batch <= 65535 && c->max_pages >= 1 && c->n_pages >= 1 &&
+           c->batch >= 1 && c->batch <= 65535 && (int64_t)c->batch * c->heads <= (1 << 20) &&
+           c->max_pages >= 1 && c->n_pages >= 1 &&
            kv_slots(*c) <= ((int64_t)1 << 30);
 }
 
@@ -40,7 +41,12 @@ bool kv_ok(const ecasq_kv_cache* c) {
 
 bool heads_ok(const ecasq_kv_cache* c, int32_t q_heads) {
     return q_heads >= c->heads && q_heads % c->heads == 0 && q_heads / c->heads <= 64 &&
-           (int64_t)c->batch * q_heads <= ((int64_t)1 << 28);
+           (int64_t)c->batch * q_heads <= (1 << 23);
+}
+
+// Per-slot work (weights, eviction): one launch covers all slots of all heads.
+bool slots_ok(const ecasq_kv_cache* c) {
+    return (int64_t)c->batch * c->heads * kv_slots(*c) <= ((int64_t)1 << 30);
 }
 
 ecasq_status status(hipError_t e) { return e == hipSuccess ? ECASQ_OK : ECASQ_EHIP; }
@@ -85,7 +91,7 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache* c, const void* new_k, int64_t 
                             const double* v_codebooks, const int32_t* v_counts, int32_t s,
                             uint64_t seed, void* k_hat, void* v_hat) {
     if (!kv_ok(c) || !new_k || !new_v || !aligned(new_k, 2) || !aligned(new_v, 2) || !starts ||
-        rows < 1 || rows > ((int64_t)1 << 30))
+        rows < 1 || rows > (1 << 23))
         return ECASQ_EINVAL;
     const int64_t row = (int64_t)c->heads * c->head_dim, most = (int64_t)1 << 30;
     if (k_stride < row || v_stride < row || k_stride > most || v_stride > most)
@@ -117,7 +123,7 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache* c, const void* new_k, int64_t 
 }
 
 size_t ecasq_kv_attention_workspace(const ecasq_kv_cache* c, int32_t q_heads, int32_t with_mass) {
-    if (!kv_sizes_ok(c) || !heads_ok(c, q_heads)) return 0;
+    if (!kv_sizes_ok(c) || !heads_ok(c, q_heads) || (with_mass && !slots_ok(c))) return 0;
     return kv_attention_bytes(*c, q_heads, with_mass != 0);
 }
 
@@ -126,7 +132,7 @@ ecasq_status ecasq_kv_attention(const ecasq_kv_cache* c, const void* q, int64_t 
                                 void* out, void* workspace, size_t workspace_bytes) {
     if (!kv_ok(c) || !heads_ok(c, q_heads) || !q || !aligned(q, 2) || !out || !aligned(out, 16) ||
         q_stride < (int64_t)q_heads * c->head_dim || q_stride > ((int64_t)1 << 40) ||
-        !std::isfinite((float)scale))
+        !std::isfinite((float)scale) || (mass_out && !slots_ok(c)))
         return ECASQ_EINVAL;
     if (!workspace || !aligned(workspace, 256)) return ECASQ_EINVAL;
     if (workspace_bytes < kv_attention_bytes(*c, q_heads, mass_out != nullptr))
@@ -137,14 +143,14 @@ ecasq_status ecasq_kv_attention(const ecasq_kv_cache* c, const void* q, int64_t 
 }
 
 size_t ecasq_kv_evict_workspace(const ecasq_kv_cache* c, int32_t keep) {
-    if (!kv_sizes_ok(c) || keep < 1) return 0;
+    if (!kv_sizes_ok(c) || !slots_ok(c) || keep < 1) return 0;
     return kv_evict_bytes(*c, keep);
 }
 
 ecasq_status ecasq_kv_evict(const ecasq_kv_cache* c, int32_t keep, int32_t recent, float* mass_out,
                             int32_t* pos_out, int32_t* lens_out, void* stream, void* workspace,
                             size_t workspace_bytes) {
-    if (!kv_ok(c) || !c->mass || !c->pos || keep < 1 || recent < 0 || recent > keep || !mass_out ||
+    if (!kv_ok(c) || !slots_ok(c) || !c->mass || !c->pos || keep < 1 || recent < 0 || recent > keep || !mass_out ||
         !pos_out || !lens_out)
         return ECASQ_EINVAL;
     if (!workspace || !aligned(workspace, 256)) return ECASQ_EINVAL;

@@ -164,3 +164,25 @@ def test_attention_of_equal_keys_is_the_mean():
     want = np.concatenate((c["v"][1, 0], c["v"][0, 0, :4])).mean(0)
     np.testing.assert_allclose(out[0], [want, want], rtol=1e-14)
     np.testing.assert_allclose(mass[0, 0], [0.1] * 20 + [0.0] * 12, rtol=1e-14)
+
+
+def test_sizes_of_one_launch():
+    """What one launch cannot cover is refused."""
+    L = ecasq.lib()
+    r = ctypes.byref(_cache(batch=65535, heads=17))
+    assert L.ecasq_kv_attention_workspace(r, 17, 0) == 0 == L.ecasq_kv_evict_workspace(r, 5)
+    c = _cache(batch=65535, heads=8, max_pages=16, page_size=128)  # 2^30 slots of heads, less 2^14
+    assert L.ecasq_kv_attention_workspace(ctypes.byref(c), 8, 1) > 0
+    assert L.ecasq_kv_attention_workspace(ctypes.byref(c), 8 * 16, 0) > 0
+    assert L.ecasq_kv_attention_workspace(ctypes.byref(c), 8 * 17, 0) == 0
+    c.max_pages = 17
+    r = ctypes.byref(c)
+    assert L.ecasq_kv_attention_workspace(r, 8, 0) > 0
+    assert L.ecasq_kv_attention_workspace(r, 8, 1) == 0 == L.ecasq_kv_evict_workspace(r, 5)
+    big = 1 << 62
+    assert L.ecasq_kv_attention(r, FAKE, 1024, 8, 1.0, FAKE, None, FAKE, FAKE,
+                                big) == ecasq.ECASQ_EINVAL
+    assert L.ecasq_kv_evict(r, 4, 1, FAKE, FAKE, FAKE, None, FAKE, big) == ecasq.ECASQ_EINVAL
+    c = _cache()
+    assert L.ecasq_kv_write(ctypes.byref(c), FAKE, 256, FAKE, 256, (1 << 23) + 1, FAKE, None, None,
+                            None, None, None, None, 0, 0, None, None) == ecasq.ECASQ_EINVAL
