@@ -206,8 +206,6 @@ __global__ __launch_bounds__(kWT) void k_kv_round(ecasq_kv_cache c, KvNew n) {
 // ---------------------------------------------------------------------------
 // Eviction
 
-constexpr int kET = 1024;
-
 // Rank of a slot: larger is kept first.  A float's bits in an order that whole
 // numbers have; NaN below all others, slots of recent positions above.
 __device__ __forceinline__ uint32_t evict_key(float mass, int32_t pos, int64_t newest_but) {
@@ -235,8 +233,8 @@ __device__ __forceinline__ int32_t wave_sums(int32_t v) {
 // again for every pass.  A long head is bounded by what one CU reads
 // and issues (32768 slots: 44 us, 13 of them until mass and pos are there), a short one by
 // the passes' latencies (640 slots: 8 us).
-constexpr int kEW = kET / 64, kBins = 2048;
-constexpr int kKeysFew = 4096, kKeysMany = 32768;
+constexpr int kBins = 2048;
+constexpr int kKeysFew = 1024, kKeysSome = 4096, kKeysMany = 32768;
 
 struct EvictPlan {
     int32_t keep, recent, moves;  // moves: the most a head can make
@@ -244,10 +242,11 @@ struct EvictPlan {
     int32_t* counts;              // per head: moves made
 };
 
-template <int KEYS>
-__global__ __launch_bounds__(kET) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
+template <int KEYS, int T>
+__global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
                                                   float* __restrict__ mass_out,
                                                   int32_t* __restrict__ pos_out) {
+    constexpr int kEW = T / 64, kEach = kBins / T;  // wavefronts; bins of a thread
     __shared__ int32_t newest;
     __shared__ uint32_t hist[3][kBins];
     __shared__ int32_t sums[3][kEW];
@@ -265,19 +264,19 @@ __global__ __launch_bounds__(kET) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     if (n <= keep) {
         if (mass_out != mass)
-            for (int32_t i = threadIdx.x; i < n; i += kET) mass_out[i] = mass[i];
+            for (int32_t i = threadIdx.x; i < n; i += T) mass_out[i] = mass[i];
         if (pos_out != pos)
-            for (int32_t i = threadIdx.x; i < n; i += kET) pos_out[i] = pos[i];
+            for (int32_t i = threadIdx.x; i < n; i += T) pos_out[i] = pos[i];
         if (threadIdx.x == 0) e.counts[blockIdx.x] = 0;
         return;
     }
-    const int32_t rounds = (n + kET - 1) / kET, first = wave * rounds * 64 + lane;
+    const int32_t rounds = (n + T - 1) / T, first = wave * rounds * 64 + lane;
     int32_t top = INT32_MIN;
     if (threadIdx.x == 0) newest = INT32_MIN;
-    for (int k = threadIdx.x; k < 3 * kBins; k += kET) hist[0][k] = 0u;
+    for (int k = threadIdx.x; k < 3 * kBins; k += T) hist[0][k] = 0u;
     // All of mass and pos at once; slots below keep go to the outputs as they are (the moves
     // overwrite the freed ones).
-    constexpr int kHeld = KEYS / kET;
+    constexpr int kHeld = KEYS / T;
     float m[KEYS ? kHeld : 1];
     const bool copy_mass = mass_out != mass, copy_pos = pos_out != pos;
     if constexpr (KEYS > 0) {
@@ -355,11 +354,15 @@ __global__ __launch_bounds__(kET) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
             if (in && (k & mask) == prefix) atomicAdd(&hist[pass][(k >> shift) & (bins - 1)], 1u);
         });
         __syncthreads();
-        // from the top: this thread's two bins, and how many slots are in those above
-        const int32_t hi = bins - 1 - 2 * (int)threadIdx.x;
-        const int32_t h1 = hi > 0 ? (int32_t)hist[pass][hi] : 0;
-        const int32_t h0 = hi > 0 ? (int32_t)hist[pass][hi - 1] : 0;
-        int32_t run = wave_sums(h1 + h0);
+        // from the top: this thread's bins, and how many slots are in those above
+        const int32_t hi = bins - 1 - kEach * (int)threadIdx.x;
+        int32_t h[kEach], own = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; k++) {
+            h[k] = hi > 0 ? (int32_t)hist[pass][hi - k] : 0;
+            own += h[k];
+        }
+        int32_t run = wave_sums(own);
         if (lane == 63) sums[pass][wave] = run;
         __syncthreads();
 #pragma unroll
@@ -367,11 +370,16 @@ __global__ __launch_bounds__(kET) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
             const int32_t v = sums[pass][w];
             run += w < wave ? v : 0;
         }
-        const int32_t above = run - h1 - h0;
+        int32_t above = run - own;
         if (above < left && left <= run) {
-            const bool second = left > above + h1;
-            found[pass][0] = second ? hi - 1 : hi;
-            found[pass][1] = left - above - (second ? h1 : 0);
+#pragma unroll
+            for (int k = 0; k < kEach; k++) {
+                if (above < left && left <= above + h[k]) {
+                    found[pass][0] = hi - k;
+                    found[pass][1] = left - above;
+                }
+                above += h[k];
+            }
         }
         __syncthreads();
         prefix |= (uint32_t)found[pass][0] << shift;
@@ -539,12 +547,16 @@ hipError_t launch_kv_evict(const ecasq_kv_cache& c, int32_t keep, int32_t recent
                            int32_t* pos_out, int32_t* lens_out, char* ws, hipStream_t st) {
     const EvictPlan e = evict_plan(c, keep, recent, ws);
     const unsigned rows = (unsigned)(c.batch * c.heads);
+    // eight wavefronts up to 1024 slots, where barriers count (329 slots: 10.4 us, 11.8 with
+    // sixteen; 2049: 14.1 and 12.9)
     if (kv_slots(c) <= kKeysFew)
-        k_kv_evict<kKeysFew><<<rows, kET, 0, st>>>(c, e, mass_out, pos_out);
+        k_kv_evict<kKeysFew, 512><<<rows, 512, 0, st>>>(c, e, mass_out, pos_out);
+    else if (kv_slots(c) <= kKeysSome)
+        k_kv_evict<kKeysSome, 1024><<<rows, 1024, 0, st>>>(c, e, mass_out, pos_out);
     else if (kv_slots(c) <= kKeysMany)
-        k_kv_evict<kKeysMany><<<rows, kET, 0, st>>>(c, e, mass_out, pos_out);
+        k_kv_evict<kKeysMany, 1024><<<rows, 1024, 0, st>>>(c, e, mass_out, pos_out);
     else
-        k_kv_evict<0><<<rows, kET, 0, st>>>(c, e, mass_out, pos_out);
+        k_kv_evict<0, 1024><<<rows, 1024, 0, st>>>(c, e, mass_out, pos_out);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     const unsigned parts = (unsigned)(e.moves < 1 ? 1 : (e.moves + kMoves - 1) / kMoves);
