@@ -227,12 +227,11 @@ __device__ __forceinline__ int32_t wave_sums(int32_t v) {
 }
 
 // The workgroup's hold on one head's keys: every wavefront has a span of consecutive
-// slots, 64 at a time, so that ranks in slot order are a ballot's and three barriers'
-// work.  The keys are in LDS (KEYS of them; in registers, 32 to a thread, the unrolled
-// passes took 17 us for the shortest heads); longer heads (KEYS = 0) read mass and pos
-// again for every pass.  A long head is bounded by what one CU reads
-// and issues (32768 slots: 44 us, 13 of them until mass and pos are there), a short one by
-// the passes' latencies (640 slots: 8 us).
+// slots, 256 at a time and four to a lane, so that ranks in slot order are four ballots'
+// and three barriers' work.  The keys are in LDS (KEYS of them); longer heads (KEYS = 0)
+// read mass and pos again for every pass.  A long head is bounded by what one CU reads and
+// issues (32768 slots: 34 us, 12 of
+// them until mass and pos are there), a short one by the passes' latencies (640 slots: 7 us).
 constexpr int kBins = 2048;
 constexpr int kKeysFew = 1024, kKeysSome = 4096, kKeysMany = 32768;
 
@@ -244,15 +243,16 @@ struct EvictPlan {
 
 template <int KEYS, int T>
 __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
-                                                  float* __restrict__ mass_out,
-                                                  int32_t* __restrict__ pos_out) {
+                                                float* __restrict__ mass_out,
+                                                int32_t* __restrict__ pos_out) {
     constexpr int kEW = T / 64, kEach = kBins / T;  // wavefronts; bins of a thread
+    constexpr int kRounds = KEYS > 4 * T ? KEYS / (4 * T) : 1;
     __shared__ int32_t newest;
     __shared__ uint32_t hist[3][kBins];
     __shared__ int32_t sums[3][kEW];
     __shared__ int32_t found[3][2];
     __shared__ int4 counts[kEW];
-    __shared__ uint32_t keys[KEYS ? KEYS : 1];
+    __shared__ uint4 keys[KEYS ? kRounds * T : 1];
     const int32_t b = blockIdx.x / c.heads;
     const int32_t slots = (int32_t)kv_slots(c), n = (int32_t)kv_len(c, b), keep = e.keep;
     const int64_t base = (int64_t)blockIdx.x * slots;
@@ -270,46 +270,62 @@ __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
         if (threadIdx.x == 0) e.counts[blockIdx.x] = 0;
         return;
     }
-    const int32_t rounds = (n + T - 1) / T, first = wave * rounds * 64 + lane;
+    // slots start + 256 r + 4 lane .. + 3 in round r
+    const int32_t rounds = (n + 4 * T - 1) / (4 * T), start = wave * rounds * 256;
+    const bool copy_mass = mass_out != mass, copy_pos = pos_out != pos;
+    auto read4 = [&](const auto* from, int32_t i, auto past, auto (&v)[4])
+                     __attribute__((always_inline)) {
+        if (i + 4 <= n) {
+            __builtin_memcpy(v, from + i, 16);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                v[u] = past;
+                if (i + u < n) v[u] = from[i + u];
+            }
+        }
+    };
+    // slots below keep go to the outputs as they are (the moves overwrite the freed ones)
+    auto copy4 = [&](auto* to, int32_t i, const auto (&v)[4]) __attribute__((always_inline)) {
+        if (i + 4 <= keep) {
+            __builtin_memcpy(to + i, v, 16);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+                if (i + u < keep) to[i + u] = v[u];
+        }
+    };
     int32_t top = INT32_MIN;
     if (threadIdx.x == 0) newest = INT32_MIN;
     for (int k = threadIdx.x; k < 3 * kBins; k += T) hist[0][k] = 0u;
-    // All of mass and pos at once; slots below keep go to the outputs as they are (the moves
-    // overwrite the freed ones).
-    constexpr int kHeld = KEYS / T;
-    float m[KEYS ? kHeld : 1];
-    const bool copy_mass = mass_out != mass, copy_pos = pos_out != pos;
+    float m[KEYS ? kRounds : 1][4];
+    int32_t p[KEYS ? kRounds : 1][4];
     if constexpr (KEYS > 0) {
-        int32_t p[kHeld];
 #pragma unroll
-        for (int r = 0; r < kHeld; r++) {
-            const int32_t i = first + 64 * r;
-            m[r] = 0.0f;
-            p[r] = INT32_MIN;
-            if (r < rounds && i < n) {
-                m[r] = mass[i];
-                p[r] = pos[i];
+        for (int r = 0; r < kRounds; r++)
+            if (r < rounds) {
+                const int32_t i = start + 256 * r + 4 * lane;
+                read4(mass, i, 0.0f, m[r]);
+                read4(pos, i, (int32_t)INT32_MIN, p[r]);
             }
-        }
 #pragma unroll
-        for (int r = 0; r < kHeld; r++) {
-            const int32_t i = first + 64 * r;
-            if (r < rounds && i < n) {
-                keys[i] = (uint32_t)p[r];
-                top = max(top, p[r]);
-                if (copy_mass && i < keep) mass_out[i] = m[r];
-                if (copy_pos && i < keep) pos_out[i] = p[r];
+        for (int r = 0; r < kRounds; r++)
+            if (r < rounds) {
+                const int32_t i = start + 256 * r + 4 * lane;
+                top = max(max(top, max(p[r][0], p[r][1])), max(p[r][2], p[r][3]));
+                if (copy_mass) copy4(mass_out, i, m[r]);
+                if (copy_pos) copy4(pos_out, i, p[r]);
             }
-        }
     } else {
-#pragma unroll 8
+#pragma unroll 2
         for (int32_t r = 0; r < rounds; r++) {
-            const int32_t i = first + 64 * r;
-            if (i < n) {
-                const int32_t v = pos[i];
-                top = max(top, v);
-                if (copy_mass && i < keep) mass_out[i] = mass[i];
-                if (copy_pos && i < keep) pos_out[i] = v;
+            const int32_t i = start + 256 * r + 4 * lane;
+            read4(pos, i, (int32_t)INT32_MIN, p[0]);
+            top = max(max(top, max(p[0][0], p[0][1])), max(p[0][2], p[0][3]));
+            if (copy_pos) copy4(pos_out, i, p[0]);
+            if (copy_mass) {
+                read4(mass, i, 0.0f, m[0]);
+                copy4(mass_out, i, m[0]);
             }
         }
     }
@@ -319,28 +335,37 @@ __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
     if (lane == 0) atomicMax(&newest, top);
     __syncthreads();
     const int64_t but = (int64_t)newest - e.recent;
+    // Slots past the end rank below or with the last (0), and behind all others of that rank:
+    // they are never among the first `keep`.
+    auto key4 = [&](int32_t i, const float (&mv)[4], const int32_t (&pv)[4])
+                    __attribute__((always_inline)) {
+        uint32_t k[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) k[u] = i + u < n ? evict_key(mv[u], pv[u], but) : 0u;
+        return make_uint4(k[0], k[1], k[2], k[3]);
+    };
     if constexpr (KEYS > 0) {  // (every lane's own slots, here and in every pass)
 #pragma unroll
-        for (int r = 0; r < kHeld; r++) {
-            const int32_t i = first + 64 * r;
-            if (r < rounds && i < n) keys[i] = evict_key(m[r], (int32_t)keys[i], but);
-        }
+        for (int r = 0; r < kRounds; r++)
+            if (r < rounds)
+                keys[wave * rounds * 64 + 64 * r + lane] =
+                    key4(start + 256 * r + 4 * lane, m[r], p[r]);
     }
-    // f(slot, key, in) for every slot of this lane; in = false past the end, so that all lanes
-    // of a wavefront meet in its ballots.  Four keys are read together.
+    // f(first slot of the wavefront's, of this lane's, the lane's four keys)
     auto each = [&](auto f) __attribute__((always_inline)) {
-        for (int32_t r = 0; r < rounds; r += 4) {
-            uint32_t k[4];
-            bool in[4];
-#pragma unroll
-            for (int u = 0; u < 4; u++) {
-                const int32_t i = first + 64 * (r + u);
-                in[u] = r + u < rounds && i < n;
-                k[u] = 0u;
-                if (in[u]) k[u] = KEYS ? keys[i] : evict_key(mass[i], pos[i], but);
+        for (int32_t r = 0; r < rounds; r++) {
+            const int32_t i0 = start + 256 * r, i = i0 + 4 * lane;
+            if (i0 >= n) break;
+            uint4 k;
+            if constexpr (KEYS > 0) {
+                k = keys[wave * rounds * 64 + 64 * r + lane];
+            } else {
+                read4(mass, i, 0.0f, m[0]);
+                read4(pos, i, (int32_t)0, p[0]);
+                k = key4(i, m[0], p[0]);
             }
-#pragma unroll
-            for (int u = 0; u < 4; u++) f(first + 64 * (r + u), k[u], in[u]);
+            const uint32_t four[4] = {k.x, k.y, k.z, k.w};
+            f(i0, i, four);
         }
     };
 
@@ -350,8 +375,11 @@ __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
 #pragma unroll
     for (int pass = 0; pass < 3; pass++) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-        each([&](int32_t, uint32_t k, bool in) {
-            if (in && (k & mask) == prefix) atomicAdd(&hist[pass][(k >> shift) & (bins - 1)], 1u);
+        each([&](int32_t, int32_t i, const uint32_t (&k)[4]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+                if ((k[u] & mask) == prefix && i + u < n)
+                    atomicAdd(&hist[pass][(k[u] >> shift) & (bins - 1)], 1u);
         });
         __syncthreads();
         // from the top: this thread's bins, and how many slots are in those above
@@ -392,14 +420,17 @@ __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
     // keep, free and move.
     {
         int4 v = {0, 0, 0, 0};
-        each([&](int32_t i, uint32_t k, bool in) {
-            const int32_t more = in && k > prefix, same = in && k == prefix;
-            if (i < keep) {
-                v.x += more;
-                v.y += same;
-            } else {
-                v.z += more;
-                v.w += same;
+        each([&](int32_t i0, int32_t i, const uint32_t (&k)[4]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int32_t more = k[u] > prefix, same = k[u] == prefix;
+                if (i0 + 256 <= keep || (i0 < keep && i + u < keep)) {
+                    v.x += more;
+                    v.y += same;
+                } else {
+                    v.z += more;
+                    v.w += same;
+                }
             }
         });
         v = {wave_sums(v.x), wave_sums(v.y), wave_sums(v.z), wave_sums(v.w)};
@@ -411,7 +442,7 @@ __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
     for (int w = 0; w < kEW; w++) {
         const int4 v = counts[w];
         const int32_t open = max(left - t, 0), low = min(v.y, open), high = min(v.w, open - low);
-        const int32_t slots_low = min(max(keep - w * rounds * 64, 0), rounds * 64);
+        const int32_t slots_low = min(max(keep - w * rounds * 256, 0), rounds * 256);
         if (w == wave) {
             ties = t;
             nf = all;
@@ -424,22 +455,38 @@ __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
     if (threadIdx.x == 0) e.counts[blockIdx.x] = all;
     const uint64_t below = (1ull << lane) - 1;
     int32_t* freed = e.lists + (int64_t)blockIdx.x * 2 * e.moves;
-    each([&](int32_t i, uint32_t k, bool in) {
-        bool on = in && k > prefix;
+    // f(u, rank) for the lane's marked slots, ranks in slot order from `from` on; all marked in
+    // the wavefront are added to it
+    auto ranked = [&](const bool (&on)[4], int32_t& from, auto f) __attribute__((always_inline)) {
+        int32_t at = from;
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const uint64_t v = __ballot(on[u]);
+            at += __popcll(v & below);
+            from += __popcll(v);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+            if (on[u]) f(u, at++);
+    };
+    each([&](int32_t i0, int32_t i, const uint32_t (&k)[4]) __attribute__((always_inline)) {
+        bool on[4], mark[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) on[u] = k[u] > prefix;
         if (some) {
-            const uint64_t tie = __ballot(in && k == prefix);
-            on |= in && k == prefix && ties + __popcll(tie & below) < left;
-            ties += __popcll(tie);
+#pragma unroll
+            for (int u = 0; u < 4; u++) mark[u] = k[u] == prefix;
+            ranked(mark, ties, [&](int u, int32_t at) { on[u] = at < left; });
         }
-        if (i - lane < keep) {  // (a wavefront's 64 slots: some below keep)
-            const uint64_t f = __ballot(in && i < keep && !on);
-            if (in && i < keep && !on) freed[nf + __popcll(f & below)] = i;
-            nf += __popcll(f);
+        if (i0 < keep) {
+#pragma unroll
+            for (int u = 0; u < 4; u++) mark[u] = i + u < keep && !on[u];
+            ranked(mark, nf, [&](int u, int32_t at) { freed[at] = i + u; });
         }
-        if (i - lane + 63 >= keep) {
-            const uint64_t v = __ballot(i >= keep && on);
-            if (i >= keep && on) freed[e.moves + nm + __popcll(v & below)] = i;
-            nm += __popcll(v);
+        if (i0 + 256 > keep) {
+#pragma unroll
+            for (int u = 0; u < 4; u++) mark[u] = i + u >= keep && on[u];
+            ranked(mark, nm, [&](int u, int32_t at) { freed[e.moves + at] = i + u; });
         }
     });
 }
