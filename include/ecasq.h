@@ -22,8 +22,9 @@
  *
  * Conventions for every entry point:
  *   - Array arguments named x, codebook*, symbols, hist, t_out, infos_dev and
- *     workspace are DEVICE pointers (HIP memory on the current device); info
- *     is a HOST pointer.  The caller owns all memory; the library never frees
+ *     workspace, and all of the serving operators' (not their descriptor of a
+ *     cache), are DEVICE pointers (HIP memory on the current device); info is a
+ *     HOST pointer.  The caller owns all memory; the library never frees
  *     caller memory.
  *   - stream is a hipStream_t passed as void* (NULL = the null stream).  All
  *     device work is ordered on it.  The solve entry points block the calling
@@ -382,8 +383,8 @@ ecasq_status ecasq_solve_batched(const void *x, ecasq_dtype dt, int64_t n, int64
  *   W[o][i] = scales[o][i / group] * c[symbols[o][i]],
  *   y[r][o] = sum_g scales[o][g] sum_{i in g} c[symbols[o][i]] x[r][i].
  * The codebook values and the scales are held in dt (ECASQ_F16 or ECASQ_BF16),
- * the type of x and y; products are exact, sums are kept in fp32 (a group's
- * first, then the groups'), y is rounded once.
+ * the type of x and y; products are exact, sums are fp32 (those of up to 128
+ * products of one scale first, times the scale, then all), y is rounded once.
  *
  * ecasq_weights_size: bytes of the packed matrix (0 unless 1 <= n_out, n_in <=
  * 2^24, n_out n_in <= 2^40 and group is a positive multiple of 32 up to 2^24; a
@@ -394,10 +395,10 @@ ecasq_status ecasq_solve_batched(const void *x, ecasq_dtype dt, int64_t n, int64
  * group) of dt; packed, device, at least ecasq_weights_size bytes (checked
  * against packed_bytes), 16-byte aligned.
  * ecasq_matvec: x, device, m rows of n_in entries x_stride >= n_in entries
- * apart, 1 <= m <= 2^20; y, device, m x n_out.  x and y need the alignment of
- * their type only.  The packed matrix is read once for every 16 rows of x.  No
- * workspace; results do not depend on the run or on m's other rows.  Both return
- * once the work is enqueued.
+ * apart, 1 <= m <= 2^20; y, device, m x n_out, outside the range from x's first
+ * entry to its last.  x and y need the alignment of their type only.  The packed
+ * matrix is read once for every 16 rows of x.  No workspace; results do not depend
+ * on the run or on m's other rows.  Both return once the work is enqueued.
  */
 size_t ecasq_weights_size(int64_t n_out, int64_t n_in, int64_t group);
 ecasq_status ecasq_weights_pack(const uint8_t *symbols, const double *codebook, int32_t t,
@@ -418,11 +419,12 @@ ecasq_status ecasq_matvec(const void *packed, ecasq_dtype dt, int64_t n_out, int
  *     (ecasq_solve_batched): 4 + 256 / head_dim bits an entry.
  * dt is ECASQ_F16 or ECASQ_BF16; head_dim 64, 128 or 256; page_size a multiple
  * of 16, 16 to 65536, and max_pages page_size at most 2^30; 1 <= heads <= 1024;
- * 1 <= batch <= 65535, batch heads at most 2^20; k, v and the books are 16-byte aligned.  lens[b] is the number of slots of sequence b in
- * use; a number below 0 counts as 0, one above max_pages page_size as that.  The
- * slots of a table entry outside [0, n_pages) hold nothing: they are not read,
- * not written, and get no weight.  A page with slots that a call writes must
- * stand in one place of the table only; a page that is only read may be shared.
+ * 1 <= batch <= 65535, batch heads at most 2^20; k, v and the books are 16-byte
+ * aligned.  lens[b] is the number of slots of sequence b in use; a number below 0
+ * counts as 0, one above max_pages page_size as that.  The slots of a table entry
+ * outside [0, n_pages) hold nothing: they are not read, not written, and get no
+ * weight.  A page with slots that a call writes must stand in one place of the
+ * table only; a page that is only read may be shared.
  *
  * mass and pos ([batch][heads][max_pages page_size], may be NULL where an entry
  * point does not need them) hold for each slot the attention weight that it has
@@ -452,8 +454,8 @@ typedef struct {
  * starts[b] .. starts[b+1]-1 are sequence b's new tokens, and lens already counts
  * them: row i goes to slot lens[b] - starts[b+1] + i (advance lens first; a
  * slot below 0 or past the table, or a row that no sequence has, is left out).
- * new_k, new_v: device, `rows` (1 to 2^23) tokens of heads x head_dim entries of dt, k_stride
- * and v_stride (>= heads head_dim) entries apart, of their type's alignment.
+ * new_k, new_v: device, `rows` (1 to 2^23) tokens of heads x head_dim entries of dt,
+ * k_stride and v_stride (>= heads head_dim) entries apart, of their type's alignment.
  * With c->mass, the slot's weight becomes 0; with c->pos, its position becomes
  * positions[i], or the slot itself where positions is NULL.
  *
@@ -484,15 +486,16 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  *   scale q[b][h] . K[b][g][t],  g = h heads / q_heads;
  * q: device, batch rows of q_heads x head_dim entries of dt, q_stride >= q_heads
  * head_dim entries apart, of their type's alignment; q_heads a multiple of heads,
- * at most 64 heads, and batch q_heads at most 2^23; out: device, batch x q_heads x head_dim of dt, 16-byte
- * aligned.  Scores, weights and sums are fp32; out is rounded once.  A sequence
- * with no slots to read, or whose scores are all -inf, gives zeros.  A NaN or
- * infinity in a row that is read reaches the result; what lies in slots past
- * lens[b] does not.
+ * at most 64 heads, and batch q_heads at most 2^23; out: device, batch x q_heads x
+ * head_dim of dt, 16-byte aligned, outside q's range.  Scores, weights and sums are fp32;
+ * out is rounded once.  A sequence with no slots to read, or whose scores are all
+ * -inf, gives zeros.
+ * A NaN or infinity in a row that is read reaches the result (an infinity as itself or
+ * as NaN); what lies in slots past lens[b] does not.
  * mass_out (device, as c->mass; NULL: no weights): for each slot below lens[b]
  * and head g, c->mass (0 where that is NULL) plus p_t summed over g's query heads
- * in order; slots past lens[b] are left as they are.  mass_out may be c->mass; with it
- * batch heads max_pages page_size is at most 2^30.
+ * in order; slots past lens[b] are left as they are.  mass_out may be c->mass; with
+ * it batch heads max_pages page_size is at most 2^30.
  * The length is split over workgroups and joined where batch and heads alone do
  * not fill the card; results are the same bit for bit from run to run.
  * workspace: at least ecasq_kv_attention_workspace bytes (0 for a bad cache or
@@ -514,10 +517,9 @@ ecasq_status ecasq_kv_attention(const ecasq_kv_cache *c, const void *q, int64_t 
  * are, and slots at or above keep may be given to another sequence after the
  * call.  mass_out, pos_out (as c->mass and c->pos, which are needed) receive the
  * slots below min(lens[b], keep), lens_out (batch) that number; they may be
- * c->mass, c->pos and c->lens.  keep >= 1, 0 <= recent <= keep, and batch heads max_pages
- * page_size at most 2^30.  Slots without
- * a page are ranked and moved like others but have no rows (a row moved from one
- * leaves the freed slot's row as it was).
+ * c->mass, c->pos and c->lens.  keep >= 1, 0 <= recent <= keep, and batch heads
+ * max_pages page_size at most 2^30.  Slots without a page are ranked and moved like
+ * others but have no rows (a row moved from one leaves the freed slot's row as it was).
  * workspace: ecasq_kv_evict_workspace bytes (0 for a bad cache or keep), 256-byte
  * aligned, as above.  Returns once the work is enqueued.
  */

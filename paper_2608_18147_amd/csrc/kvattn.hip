@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache
 #pragma unroll
                 for (int j = 0; j < J; j++) s[t] = mfma<DT>(kv[t][j], qv[j], s[t]);
             }
-            if (tile[0].live < 16 || tile[1].live < 16) {  // slots that hold nothing: no NaN of theirs
+            if (tile[0].live < 16 || tile[1].live < 16) {  // no NaN of slots that hold nothing
 #pragma unroll
                 for (int k = 0; k < 8; k++)
                     if (4 * g + k % 4 >= tile[k / 4].live)

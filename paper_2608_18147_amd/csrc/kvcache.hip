@@ -161,10 +161,10 @@ __global__ __launch_bounds__(kWT) void k_kv_round(ecasq_kv_cache c, KvNew n) {
                                 : __builtin_nanf("");
                 B.h[k] = h;
                 if (k == 0) B.t = t;
-                if (part == 0)
-                    static_cast<uint16_t*>(value ? c.v_books
-                                                 : c.k_books)[(row0 + (int64_t)r * c.page_size) * 16 +
-                                                              k] = h;
+                if (part == 0) {
+                    auto* to = static_cast<uint16_t*>(value ? c.v_books : c.k_books);
+                    to[(row0 + (int64_t)r * c.page_size) * 16 + k] = h;
+                }
             }
             __builtin_amdgcn_wave_barrier();
         }
@@ -230,8 +230,7 @@ __device__ __forceinline__ int32_t wave_sums(int32_t v) {
 // slots, 256 at a time and four to a lane, so that ranks in slot order are four ballots'
 // and three barriers' work.  The keys are in LDS (KEYS of them); longer heads (KEYS = 0)
 // read mass and pos again for every pass.  A long head is bounded by what one CU reads and
-// issues (32768 slots: 34 us, 12 of
-// them until mass and pos are there), a short one by the passes' latencies (640 slots: 7 us).
+// issues (32768 slots: 34 us), a short one by the passes' latencies (640 slots: 7 us).
 constexpr int kBins = 2048;
 constexpr int kKeysFew = 1024, kKeysSome = 4096, kKeysMany = 32768;
 

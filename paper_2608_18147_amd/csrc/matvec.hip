@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
         const int64_t row = t < p.tiles ? t : p.tiles - 1;
         const int32_t u = 4 * NB * c + n16;
         const int32_t k = p.unit_shift >= 0 ? u >> p.unit_shift : u / p.unit;
-        uint2 v = {0u, 0u};  // past the matrix: of x and of the symbols' values, which are 0 and finite
+        uint2 v = {0u, 0u};  // past the matrix, where x is 0 and the symbols' values are finite
         if (k < p.groups)
             v = *reinterpret_cast<const uint2*>(p.packed + p.scales_at +
                                                 (row * p.groups + k) * 32 + g * 8);

@@ -49,6 +49,12 @@ bool slots_ok(const ecasq_kv_cache* c) {
     return (int64_t)c->batch * c->heads * kv_slots(*c) <= ((int64_t)1 << 30);
 }
 
+// Do `rows` rows of `row` 16-bit entries, a_stride apart at a, meet n at b?
+bool overlap(const void* a, int64_t rows, int64_t row, int64_t a_stride, const void* b, int64_t n) {
+    const auto a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    return a0 < b0 + 2 * (uintptr_t)n && b0 < a0 + 2 * ((uintptr_t)(rows - 1) * a_stride + row);
+}
+
 ecasq_status status(hipError_t e) { return e == hipSuccess ? ECASQ_OK : ECASQ_EHIP; }
 
 }  // namespace
@@ -78,7 +84,8 @@ ecasq_status ecasq_matvec(const void* packed, ecasq_dtype dt, int64_t n_out, int
                           void* y) {
     if (!packed || !aligned(packed, 16) || !half_type(dt) || !weights_ok(n_out, n_in, group) ||
         !x || !y || !aligned(x, 2) || !aligned(y, 2) || m < 1 || m > ((int64_t)1 << 20) ||
-        x_stride < n_in || x_stride > ((int64_t)1 << 40))
+        x_stride < n_in || x_stride > ((int64_t)1 << 40) ||
+        overlap(x, m, n_in, x_stride, y, m * n_out))
         return ECASQ_EINVAL;
     return status(launch_matvec(static_cast<const char*>(packed), dt, Weights{n_out, n_in, group},
                                 x, m, x_stride, y, static_cast<hipStream_t>(stream)));
@@ -132,11 +139,13 @@ ecasq_status ecasq_kv_attention(const ecasq_kv_cache* c, const void* q, int64_t 
                                 void* out, void* workspace, size_t workspace_bytes) {
     if (!kv_ok(c) || !heads_ok(c, q_heads) || !q || !aligned(q, 2) || !out || !aligned(out, 16) ||
         q_stride < (int64_t)q_heads * c->head_dim || q_stride > ((int64_t)1 << 40) ||
-        !std::isfinite((float)scale) || (mass_out && !slots_ok(c)))
+        !std::isfinite((float)scale * 1.5f) || (mass_out && !slots_ok(c)))
         return ECASQ_EINVAL;
     if (!workspace || !aligned(workspace, 256)) return ECASQ_EINVAL;
     if (workspace_bytes < kv_attention_bytes(*c, q_heads, mass_out != nullptr))
         return ECASQ_EWORKSPACE;
+    const int64_t row = (int64_t)q_heads * c->head_dim;
+    if (overlap(q, c->batch, row, q_stride, out, c->batch * row)) return ECASQ_EINVAL;
     return status(launch_kv_attention(*c, q, q_stride, q_heads, (float)scale, mass_out, out,
                                       static_cast<char*>(workspace),
                                       static_cast<hipStream_t>(stream)));
@@ -150,8 +159,8 @@ size_t ecasq_kv_evict_workspace(const ecasq_kv_cache* c, int32_t keep) {
 ecasq_status ecasq_kv_evict(const ecasq_kv_cache* c, int32_t keep, int32_t recent, float* mass_out,
                             int32_t* pos_out, int32_t* lens_out, void* stream, void* workspace,
                             size_t workspace_bytes) {
-    if (!kv_ok(c) || !slots_ok(c) || !c->mass || !c->pos || keep < 1 || recent < 0 || recent > keep || !mass_out ||
-        !pos_out || !lens_out)
+    if (!kv_ok(c) || !slots_ok(c) || !c->mass || !c->pos || keep < 1 || recent < 0 ||
+        recent > keep || !mass_out || !pos_out || !lens_out)
         return ECASQ_EINVAL;
     if (!workspace || !aligned(workspace, 256)) return ECASQ_EINVAL;
     if (workspace_bytes < kv_evict_bytes(*c, keep)) return ECASQ_EWORKSPACE;

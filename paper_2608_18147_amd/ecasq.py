@@ -555,22 +555,26 @@ def ecasq_matvec(w, x, out=None, stream=None):
     """y = W x for every row of x [..., n_in]; returns y [..., n_out]."""
     if not isinstance(x, torch.Tensor) or x.dtype != w.dtype or x.device != w.device:
         raise TypeError(f"x must be a {w.dtype} tensor on {w.device}")
-    if x.dim() == 0 or x.shape[-1] != w.n_in:
+    shape = x.shape
+    if not shape or shape[-1] != w.n_in:
         raise ValueError(f"x must end in {w.n_in} entries")
     if out is not None:
-        _tensor(out, "out", w.dtype, w.device, x.shape[:-1] + (w.n_out,))
-    return _run(_matvec, w.device, stream, w, x, out)
+        _tensor(out, "out", w.dtype, w.device, shape[:-1] + (w.n_out,))
+    return _run(_matvec, w.device, stream, w, x, shape, out)
 
 
-def _matvec(st, w, x, out):
-    n_in, shape = w.n_in, x.shape[:-1] + (w.n_out,)
-    if x.dim() == 2 and x.stride(1) == 1 and x.stride(0) >= n_in:
-        m, step = x.shape[0], x.stride(0)
+def _matvec(st, w, x, shape, out):
+    n_in = w.n_in
+    if len(shape) == 2 and (x.is_contiguous() or (x.stride(1) == 1 and x.stride(0) >= n_in)):
+        m = shape[0]
+        step = x.stride(0) if m > 1 else n_in
+        if out is None:
+            out = x.new_empty((m, w.n_out))
     else:
         x = x.reshape(-1, n_in).contiguous()
         m, step = x.shape[0], n_in
-    if out is None:
-        out = x.new_empty(shape)
+        if out is None:
+            out = x.new_empty(shape[:-1] + (w.n_out,))
     if m:
         _raise(lib().ecasq_matvec(w.packed.data_ptr(), _HALF[w.dtype], w.n_out, n_in, w.group,
                                   x.data_ptr(), m, step, st, out.data_ptr()))
@@ -618,6 +622,7 @@ class ecasq_kv_cache:
                              *[x.data_ptr() if x is not None else None for x in
                                (k, v, k_books, v_books, table, lens, mass, pos)])
         self._ref = ctypes.byref(self._c)
+        self._unused = table.new_empty(256, dtype=torch.uint8)
         self._sizes = {}
 
     def __setattr__(self, name, value):
@@ -626,7 +631,8 @@ class ecasq_kv_cache:
         self.__dict__[name] = value
 
     def _workspace(self, name, *args):
-        """A workspace of the size that the library's function `name` says."""
+        """A workspace of the size that the library's function `name` says (256 bytes:
+        the call needs none, and any will do)."""
         key = (name,) + args
         size = self._sizes.get(key)
         if size is None:
@@ -634,6 +640,8 @@ class ecasq_kv_cache:
             if size == 0:
                 raise EcasqError(ECASQ_EINVAL)
             self._sizes[key] = size
+        if size <= 256:
+            return self._unused, size
         return self.table.new_empty(size, dtype=torch.uint8), size
 
 
@@ -721,6 +729,9 @@ def ecasq_kv_evict(kv, keep, recent=0, mass_out=None, pos_out=None, lens_out=Non
     those of the `recent` newest positions and the largest mass; the kept rows
     are moved below slot `keep`.  kv.mass, kv.pos and kv.lens are updated, or the
     tensors given for them in their place."""
+    keep, recent = int(keep), int(recent)
+    if not -2 ** 31 <= keep < 2 ** 31 or not -2 ** 31 <= recent < 2 ** 31:
+        raise ValueError("keep and recent must be 32-bit integers")
     if kv.mass is None or kv.pos is None:
         raise ValueError("the cache needs mass and pos")
     mass_out = kv.mass if mass_out is None else \
@@ -729,7 +740,7 @@ def ecasq_kv_evict(kv, keep, recent=0, mass_out=None, pos_out=None, lens_out=Non
         _tensor(pos_out, "pos_out", torch.int32, kv.device, kv._slots_shape)
     lens_out = kv.lens if lens_out is None else \
         _tensor(lens_out, "lens_out", torch.int32, kv.device, (kv.batch,))
-    _run(_evict, kv.device, stream, kv, int(keep), int(recent), mass_out, pos_out, lens_out)
+    _run(_evict, kv.device, stream, kv, keep, recent, mass_out, pos_out, lens_out)
 
 
 def _evict(st, kv, keep, recent, mass_out, pos_out, lens_out):
