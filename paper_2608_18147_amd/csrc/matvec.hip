@@ -7,46 +7,81 @@
 namespace ecasq {
 namespace {
 
-// One dword of symbols, one scale or one codebook value per thread.
+// Eight symbols' bytes to a dword; a symbol of t or more counts as t - 1.
+__device__ __forceinline__ uint32_t pack8(const uint32_t (&b)[2], uint32_t t) {
+    // (no carries: a byte's low seven bits plus 128 - t stay below 256)
+    const uint32_t add = (0x80u - t) * 0x01010101u;
+    const uint32_t over = (((b[0] & 0x7F7F7F7Fu) + add) | b[0] | ((b[1] & 0x7F7F7F7Fu) + add) |
+                           b[1]) & 0x80808080u;
+    uint32_t v = 0;
+    if (over == 0u) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const uint32_t two = (b[k] | b[k] >> 4) & 0x00FF00FFu;
+            v |= ((two | two >> 8) & 0xFFFFu) << (16 * k);
+        }
+        return v;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t s = b[i / 4] >> (i % 4 * 8) & 0xFFu;
+        v |= (s < t ? s : t - 1u) << (4 * i);
+    }
+    return v;
+}
+
+// A wavefront per tile of 16 rows and block of 128 columns, 16 bytes a lane: every line that
+// it reads is read whole (28672 x 8192, 356 MB read and written: 265 us with a dword a
+// thread and its place by 64-bit divisions, 68 so).  Then a scale or a codebook value a thread.
 template <int DT>
 __global__ __launch_bounds__(256) void k_weights_pack(const uint8_t* __restrict__ sym,
                                                       const double* __restrict__ cb, int32_t t,
                                                       const uint16_t* __restrict__ scales,
                                                       Weights w, char* __restrict__ packed) {
-    const int64_t nw = w.tiles() * w.blocks() * 256, ns = w.tiles() * w.groups() * 16;
+    const int lane = threadIdx.x % 64;
+    const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int32_t blocks = (int32_t)w.blocks();
+    const int64_t units = w.tiles() * blocks;  // below 2^30
     // What fills up tiles and blocks meets zeros of x and is not to make NaN of them: a
     // symbol whose value is finite (0 if there is none).
     uint32_t pad = 0;
     for (int k = 15; k >= 0; k--)
         if (k < t && __builtin_isfinite(from16<DT>(to16<DT>(cb[k])))) pad = (uint32_t)k;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < nw + ns + kWHead / 2;
-         at += (int64_t)gridDim.x * 256) {
-        if (at < nw) {
-            const int l = (int)(at / 4 % 64), j = (int)(at % 4);
-            const int64_t block = at / 256;
-            const int64_t o = block / w.blocks() * 16 + l % 16;
-            const int64_t i0 = block % w.blocks() * 128 + 32 * j + 8 * (l / 16);
-            uint8_t eight[8];
-            const bool whole = o < w.n_out && i0 + 8 <= w.n_in;
-            if (whole) __builtin_memcpy(eight, sym + o * w.n_in + i0, 8);
-            uint32_t v = 0;
+    for (int32_t u = (int32_t)blockIdx.x * 4 + wave; u < units; u += (int32_t)gridDim.x * 4) {
+        const int32_t tile = u / blocks, block = u - tile * blocks;
+        const int64_t o = (int64_t)tile * 16 + lane % 16;
+        const int32_t i0 = block * 128 + 8 * (lane / 16);
+        const uint8_t* from = sym + o * w.n_in + i0;
+        uint32_t bytes[4][2];
+        if (o < w.n_out && block * 128 + 128 <= w.n_in) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                uint32_t s = pad;
-                if (o < w.n_out && i0 + i < w.n_in) {
-                    s = whole ? eight[i] : sym[o * w.n_in + i0 + i];
-                    s = s < (uint32_t)t ? s : (uint32_t)t - 1u;
+            for (int j = 0; j < 4; j++) __builtin_memcpy(bytes[j], from + 32 * j, 8);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                bytes[j][0] = bytes[j][1] = 0u;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    uint32_t s = pad;
+                    if (o < w.n_out && i0 + 32 * j + i < w.n_in) s = from[32 * j + i];
+                    bytes[j][i / 4] |= s << (i % 4 * 8);
                 }
-                v |= s << (4 * i);
             }
-            reinterpret_cast<uint32_t*>(packed + kWHead)[at] = v;
-        } else if (at < nw + ns) {
-            const int64_t k = at - nw, o = k / 16 / w.groups() * 16 + k % 16;
+        }
+        const uint4 v = {pack8(bytes[0], (uint32_t)t), pack8(bytes[1], (uint32_t)t),
+                         pack8(bytes[2], (uint32_t)t), pack8(bytes[3], (uint32_t)t)};
+        reinterpret_cast<uint4*>(packed + kWHead)[(int64_t)u * 64 + lane] = v;
+    }
+    const int64_t ns = w.tiles() * w.groups() * 16;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < ns + kWHead / 2;
+         k += (int64_t)gridDim.x * 256) {
+        if (k < ns) {
+            const int64_t o = k / 16 / w.groups() * 16 + k % 16;
             reinterpret_cast<uint16_t*>(packed + w.scales_at())[k] =
                 o < w.n_out ? scales[o * w.groups() + k / 16 % w.groups()] : (uint16_t)0;
         } else {
-            const int64_t k = at - nw - ns;
-            reinterpret_cast<uint16_t*>(packed)[k] = k < t ? to16<DT>(cb[k]) : (uint16_t)0;
+            const int64_t at = k - ns;
+            reinterpret_cast<uint16_t*>(packed)[at] = at < t ? to16<DT>(cb[at]) : (uint16_t)0;
         }
     }
 }
@@ -327,8 +362,8 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
 hipError_t launch_weights_pack(const uint8_t* symbols, const double* codebook, int32_t t,
                                const void* scales, int dt, const Weights& w, char* packed,
                                hipStream_t st) {
-    const int64_t n = w.bytes() / 4;
-    const unsigned g = (unsigned)(n < ((int64_t)1 << 28) ? (n + 255) / 256 : (int64_t)1 << 20);
+    const int64_t n = (w.tiles() * w.blocks() + 3) / 4;
+    const unsigned g = (unsigned)(n < 4096 ? n : 4096);  // twice what is resident at once
     const auto* sc = static_cast<const uint16_t*>(scales);
     if (dt == ECASQ_F16)
         k_weights_pack<1><<<g, 256, 0, st>>>(symbols, codebook, t, sc, w, packed);
