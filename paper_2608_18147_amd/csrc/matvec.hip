@@ -140,7 +140,27 @@ struct MatvecArgs {
     int32_t parts;             // S
     int32_t slots;             // tiles that a workgroup has at a time
     int32_t turns;             // MANY: tiles for which a part of x is kept
+    int32_t odd;               // many rows of x, some of which begin between two dwords
 };
+
+// Eight entries of a row of x, some of whose rows begin between two dwords (odd, the same for
+// all lanes).  Loads that begin there take a lane after the other: the dwords begin an entry
+// early then, but for the row's first entry, in front of which nothing may be.
+__device__ __forceinline__ u32x4 load8(const uint16_t* p, int32_t odd, bool first) {
+    u32x4 v;
+    if (!odd || first) {
+        __builtin_memcpy(&v, p, 16);
+        return v;
+    }
+    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 2u;
+    uint32_t w[4];
+    __builtin_memcpy(w, __builtin_assume_aligned(reinterpret_cast<const char*>(p) - off, 4), 16);
+    const uint32_t last = p[7];
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+        v[k] = __builtin_amdgcn_alignbyte(k < 3 ? w[k + 1] : last, w[k], off);
+    return v;
+}
 constexpr int kTurns = 4, kXBytes = 65536;
 
 // A wavefront has one chunk; or several (then S is 16 and a workgroup has one tile at a
@@ -195,7 +215,7 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
 #pragma unroll
             for (int k = 0; k < 4 * NB; k++) {
                 x[k] = u32x4{0u, 0u, 0u, 0u};
-                if (has) __builtin_memcpy(&x[k], xr + i0 + 32 * k, 16);
+                if (has) x[k] = load8(xr + i0 + 32 * k, p.odd, i0 + 32 * k == 0);
             }
             return;
         }
@@ -212,7 +232,9 @@ __global__ __launch_bounds__(kMT) void k_matvec(MatvecArgs p) {
         for (int k = 0; k < 4 * NB; k++) {
             x[k] = u32x4{0u, 0u, 0u, 0u};
             if (32 * (k + 1) <= left) {
-                if (has) __builtin_memcpy(&x[k], xr + i0 + 32 * k, 16);
+                // (several chunks: one in three or more, and the registers are full)
+                if (has)
+                    x[k] = load8(xr + i0 + 32 * k, MODE == kMany ? 0 : p.odd, i0 + 32 * k == 0);
             } else if (32 * k < left) {
                 x[k] = edge;
             }
@@ -435,6 +457,8 @@ hipError_t launch_matvec(const char* packed, int dt, const Weights& w, const voi
     for (int64_t r0 = 0; r0 < m; r0 += most) {
         const int64_t rows = m - r0 < most ? m - r0 : most;
         a.x = static_cast<const uint16_t*>(x) + r0 * x_stride;
+        // (8191 x 4096 for 12 rows 26 us, 16 so; 4101 x 11000 for 5 rows 11.8 and 12.8)
+        a.odd = rows > 5 && (reinterpret_cast<uintptr_t>(a.x) % 4 != 0 || x_stride % 2 != 0);
         a.y = static_cast<uint16_t*>(y) + r0 * w.n_out;
         a.m = (int32_t)rows;
         const dim3 g((unsigned)(wgs < cus ? wgs : cus), (unsigned)((rows + 15) / 16));
