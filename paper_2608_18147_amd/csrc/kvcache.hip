@@ -493,6 +493,7 @@ __global__ __launch_bounds__(T) void k_kv_evict(ecasq_kv_cache c, EvictPlan e,
 // The moves, 64 of a head to a workgroup: where each goes from and to, then the rows
 // (and their codebooks) in pieces of 16 bytes.
 constexpr int kMoves = 64, kVT = 256;
+typedef uint32_t Piece __attribute__((ext_vector_type(4)));
 
 __global__ __launch_bounds__(kVT) void k_kv_move(ecasq_kv_cache c, EvictPlan e, float* mass_out,
                                                  int32_t* pos_out, int32_t* lens_out) {
@@ -519,19 +520,27 @@ __global__ __launch_bounds__(kVT) void k_kv_move(ecasq_kv_cache c, EvictPlan e, 
     __syncthreads();
     const int32_t piece = c.coded ? c.head_dim / 32 : c.head_dim / 8;  // of a row
     const int32_t books = c.coded ? 2 : 0, each = 2 * (piece + books);
-    for (int32_t k = threadIdx.x; k < count * each; k += kVT) {
-        const int32_t m = k / each;
-        int32_t u = k % each;
-        if (to[m] < 0) continue;
-        const bool value = u >= piece + books;
-        if (value) u -= piece + books;
-        if (u < piece) {
-            uint4* x = static_cast<uint4*>(value ? c.v : c.k);
-            x[to[m] * piece + u] = x[from[m] * piece + u];
-        } else {
-            uint4* x = static_cast<uint4*>(value ? c.v_books : c.k_books);
-            x[to[m] * 2 + u - piece] = x[from[m] * 2 + u - piece];
+    // A thread keeps its piece of a row for all moves, with four of them on the way at a time (no
+    // row is read that another move writes); 1304 of 8 heads of 256 in 16 bits: 21 us by the
+    // call with one, 17 so.
+    const int32_t per = kVT / each, u0 = threadIdx.x % each;
+    const bool value = u0 >= piece + books;
+    const int32_t u1 = value ? u0 - piece - books : u0;
+    const bool book = u1 >= piece;
+    const int32_t size = book ? 2 : piece, u = book ? u1 - piece : u1;
+    Piece* x = static_cast<Piece*>(book ? value ? c.v_books : c.k_books : value ? c.v : c.k) + u;
+    for (int32_t m = threadIdx.x / each; m < count && threadIdx.x < per * each; m += 4 * per) {
+        Piece v[4];
+        int64_t at[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {  // (past the last or without a page: row 0, not written)
+            const int32_t k = min(m + i * per, kMoves - 1);
+            at[i] = m + i * per < count ? to[k] : -1;
+            v[i] = x[(at[i] < 0 ? 0 : from[k]) * size];
         }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (at[i] >= 0) x[at[i] * size] = v[i];
     }
 }
 
