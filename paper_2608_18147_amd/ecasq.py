@@ -485,7 +485,7 @@ def _tensor(x, name, dtype, device, shape=None):
     """x, once it is seen to be a contiguous tensor as the library needs it."""
     if not isinstance(x, torch.Tensor) or x.dtype != dtype or x.device != device:
         raise TypeError(f"{name} must be a {dtype} tensor on {device}")
-    if shape is not None and tuple(x.shape) != tuple(shape):
+    if shape is not None and x.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}")
     if not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
