@@ -524,7 +524,7 @@ size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 // they seldom are of one length (131071 coded slots alone: 54 us with 1024, 60 with
 // 1792; 16 sequences of 0 to 8191: 49 and 39 us; 64 of 3500 to 4500 in 16 bits: 190 and
 // 193 us).  A chunk has 256 slots at least: two rounds of a workgroup take less than
-// the launch that joins two chunks (4 sequences of up to 200: 6.9 us, 8.5 with 128); 128 where
+// the launch that joins two chunks (4 sequences of up to 200: 6.1 us, 7.9 with 128); 128 where
 // there are chunks to join anyway, few workgroups otherwise and few chunks to a head (8 heads of
 // 3000 coded slots: 96 workgroups, 9.1 us and 10.3 with 256; 8 heads of 8000 slots: 250, 14.3
 // and 12.7; one head of 45000: 18.5 and 15.1).

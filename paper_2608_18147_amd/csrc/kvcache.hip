@@ -602,8 +602,8 @@ hipError_t launch_kv_evict(const ecasq_kv_cache& c, int32_t keep, int32_t recent
                            int32_t* pos_out, int32_t* lens_out, char* ws, hipStream_t st) {
     const EvictPlan e = evict_plan(c, keep, recent, ws);
     const unsigned rows = (unsigned)(c.batch * c.heads);
-    // eight wavefronts up to 1024 slots, where barriers count (329 slots: 10.4 us, 11.8 with
-    // sixteen; 2049: 14.1 and 12.9)
+    // eight wavefronts up to 1024 slots, where barriers count (347 slots: 10.3 us, 11.3 with
+    // sixteen; 2347: 14.1 and 13.2)
     if (kv_slots(c) <= kKeysFew)
         k_kv_evict<kKeysFew, 512><<<rows, 512, 0, st>>>(c, e, mass_out, pos_out);
     else if (kv_slots(c) <= kKeysSome)
