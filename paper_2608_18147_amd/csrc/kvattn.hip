@@ -413,11 +413,12 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache
             __builtin_assume_aligned(part + (row * p.chunks + ch) * D + quad * E, 16), o, 4 * E);
         return;
     }
-    const float by = L == 0.0f ? 0.0f : 1.0f / L;
+    const float by = 1.0f / L;
     uint32_t w[E / 2];
 #pragma unroll
-    for (int i = 0; i < E / 2; i++)
-        w[i] = to16<DT>(o[2 * i] * by) | (uint32_t)to16<DT>(o[2 * i + 1] * by) << 16;
+    for (int i = 0; i < E / 2; i++)  // (no weight at all: zeros, whatever the values are)
+        w[i] = L == 0.0f ? 0u
+                         : to16<DT>(o[2 * i] * by) | (uint32_t)to16<DT>(o[2 * i + 1] * by) << 16;
     __builtin_memcpy(__builtin_assume_aligned(out + row * D + quad * E, 8), w, 2 * E);
 }
 
@@ -460,6 +461,7 @@ __device__ __forceinline__ void join_row(const Plan& p, int64_t row, int32_t use
     if (side != 0) return;
 #pragma unroll
     for (int k = 1; k < kSide; k++) o += sums[k * (D / 4) + e];
+    if (all.y == 0.0f) o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // no weight at all
     const float by = all.y == 0.0f ? 0.0f : 1.0f / all.y;
     const uint32_t w[2] = {to16<DT>(o[0] * by) | (uint32_t)to16<DT>(o[1] * by) << 16,
                            to16<DT>(o[2] * by) | (uint32_t)to16<DT>(o[3] * by) << 16};
