@@ -490,8 +490,11 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  * head_dim of dt, 16-byte aligned, outside q's range.  Scores, weights and sums are fp32;
  * out is rounded once.  A sequence with no slots to read, or whose scores are all
  * -inf, gives zeros.
- * A NaN or infinity in a row that is read reaches the result (an infinity as itself or
- * as NaN); what lies in slots past lens[b] does not.
+ * Otherwise a NaN or an infinity in a row that is read reaches the result as the formula says:
+ * an infinite value as itself however small its weight is, as NaN where it meets one of the other
+ * sign or its score is -inf; what lies in slots past lens[b] does not.  Finite values give finite
+ * results.  Where infinities or values near the type's largest are met, a part of the call
+ * takes many times as long.
  * mass_out (device, as c->mass; NULL: no weights): for each slot below lens[b]
  * and head g, c->mass (0 where that is NULL) plus p_t summed over g's query heads
  * in order; slots past lens[b] are left as they are.  mass_out may be c->mass; with

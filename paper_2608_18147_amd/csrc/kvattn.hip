@@ -13,7 +13,11 @@
 // stay below 2^15 in f16, 2^8 in bf16, and the sums are fp32), so that the four
 // lanes of a head seldom have to agree on a new one.  Weights enter the second
 // product as two 16-bit numbers, rounded and remainder: one alone would add an
-// error as large as the result's own rounding.
+// error as large as the result's own rounding.  Neither part may meet an infinity (a
+// remainder is 0 or, in bf16, of either sign; a small weight of f16 is 0 in both), and bf16
+// values near the largest pass the floats before they are divided by the sum: where a
+// result is no finite number though the sum of the weights is, the wavefront takes it again
+// from the definition (by_definition).
 #include "half16.hpp"
 #include "serve.hpp"
 
@@ -130,6 +134,58 @@ struct Tile {
 // bytes each, so that the groups' reads meet different banks and every address
 // is a byte (the symbol's, with the group's bits) and a constant high byte.
 constexpr int kBookBytes = 1280;
+
+template <int DT, bool CODED, int D>
+__device__ __forceinline__ float entry(const void* rows, const void* books, int64_t row, int e) {
+    if constexpr (CODED) {
+        const uint32_t two = static_cast<const uint8_t*>(rows)[row * (D / 2) + e / 2];
+        return from16<DT>(
+            static_cast<const uint16_t*>(books)[row * 16 + (two >> (e % 2 * 4) & 15u)]);
+    } else {
+        return from16<DT>(static_cast<const uint16_t*>(rows)[row * D + e]);
+    }
+}
+
+// o = sum_t p_t V_t over the slots lo .. end - 1, entries E quad and up of a head, for the 16
+// consecutive lanes `quad` of each of a wavefront's four heads: scores of 16 slots by a lane each,
+// then weights p = 2^(score - up) by (at most 1, so sums of finite values are finite), slot after
+// slot.  The smallest float is added to a weight, so that it is no 0 by underflow: that makes an
+// infinity of an infinity and nothing of a finite value; a score of -inf has weight 0, and 0
+// times an infinity is NaN.  A path for rare values, not for speed (64 sequences of about 4000
+// 16-bit slots with one infinity each: 1.4 ms, 0.19 with none).
+template <int DT, bool CODED, int D>
+__device__ __forceinline__ void by_definition(const ecasq_kv_cache& c, int32_t b, int32_t head,
+                                              const uint16_t* __restrict__ q, int32_t lo,
+                                              int32_t end, float scale, float up, float by,
+                                              float (&o)[D / 16]) {
+    constexpr int E = D / 16;
+    const int lane = threadIdx.x % 64, quad = lane % 16;
+#pragma unroll
+    for (int i = 0; i < E; i++) o[i] = 0.0f;
+#pragma unroll 1
+    for (int32_t s0 = lo; s0 < end; s0 += 16) {
+        const int64_t mine = s0 + quad < end ? kv_row(c, b, head, s0 + quad) : -1;
+        float z = 0.0f;
+        if (mine >= 0)
+#pragma unroll 8
+            for (int e = 0; e < D; e++)
+                z = __builtin_fmaf(entry<DT, CODED, D>(c.k, c.k_books, mine, e), from16<DT>(q[e]),
+                                   z);
+        z *= scale;
+#pragma unroll 1
+        for (int k = 0; k < 16; k++) {
+            const float score = __shfl(z, lane - quad + k);
+            const int64_t row = s0 + k < end ? kv_row(c, b, head, s0 + k) : -1;
+            if (row < 0) continue;
+            const float weight = __builtin_fmaf(__builtin_amdgcn_exp2f(score - up), by,
+                                                score > -INFINITY ? 0x1p-149f : 0.0f);
+#pragma unroll
+            for (int i = 0; i < E; i++)
+                o[i] = __builtin_fmaf(
+                    weight, entry<DT, CODED, D>(c.v, c.v_books, row, quad * E + i), o[i]);
+        }
+    }
+}
 
 template <int DT, bool CODED, int D>
 __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache c, Plan p,
@@ -406,6 +462,23 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache
         for (int w = 0; w < kWaves; w++)
             o[i] += from[w * kPart + i * 256 + threadIdx.x] * down[w];
     }
+    // (no weight at all: 0, or the NaN of the values, which a join hands on)
+    const float by = L == 0.0f ? 1.0f : 1.0f / L;
+    float none = 0.0f;  // NaN if one of the entries is no finite number
+#pragma unroll
+    for (int i = 0; i < E; i++) {
+        none += o[i] * 0.0f;
+        o[i] *= by;
+    }
+    const bool again = none != 0.0f && L > 0.0f && L < INFINITY;
+    if (__any(again)) {  // (heads are the group's: the others' threads have returned)
+        float exact[E];
+        by_definition<DT, CODED, D>(
+            c, b, head, q + (int64_t)b * q_stride + ((int64_t)head * p.group + ht * 16 + o16) * D, lo,
+            end, scale, M - kLift<DT>, by, exact);
+#pragma unroll
+        for (int i = 0; i < E; i++) o[i] = again ? exact[i] : o[i];
+    }
     const int64_t row = ((int64_t)b * c.heads + head) * p.group + ht * 16 + o16;
     if (ml && quad == 0) ml[row * p.chunks + ch] = make_float2(M, L);
     if (used > 1) {
@@ -413,12 +486,10 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache
             __builtin_assume_aligned(part + (row * p.chunks + ch) * D + quad * E, 16), o, 4 * E);
         return;
     }
-    const float by = 1.0f / L;
     uint32_t w[E / 2];
 #pragma unroll
     for (int i = 0; i < E / 2; i++)  // (no weight at all: zeros, whatever the values are)
-        w[i] = L == 0.0f ? 0u
-                         : to16<DT>(o[2 * i] * by) | (uint32_t)to16<DT>(o[2 * i + 1] * by) << 16;
+        w[i] = L == 0.0f ? 0u : to16<DT>(o[2 * i]) | (uint32_t)to16<DT>(o[2 * i + 1]) << 16;
     __builtin_memcpy(__builtin_assume_aligned(out + row * D + quad * E, 8), w, 2 * E);
 }
 
@@ -427,7 +498,8 @@ __global__ __launch_bounds__(kAT, D == 256 ? 2 : 3) void k_attend(ecasq_kv_cache
 // key/value head at a time: the sum over the group's heads in order.
 constexpr int kJT = 256, kSpan = 4 * kJT;
 
-// Maximum and sum of a head's chunks, by one wavefront; the same for every lane.
+// Maximum and sum of a head's chunks, by one wavefront; the same for every lane.  (A chunk's
+// part is divided by its sum already.)
 __device__ __forceinline__ float2 joined(const float2* __restrict__ ml, int32_t used) {
     const int lane = threadIdx.x % 64;
     float m = -INFINITY, l = 0.0f;
@@ -452,19 +524,24 @@ __device__ __forceinline__ void join_row(const Plan& p, int64_t row, int32_t use
     const float2* at = ml + row * p.chunks;
     const float2 all = joined(at, used);
     const auto* from = reinterpret_cast<const f32x4*>(part + row * p.chunks * D) + e;
+    const float by = 1.0f / all.y;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int32_t k = side; k < used; k += kSide)
-        o += from[(int64_t)k * (D / 4)] * down_to(at[k].x, all.x);
+    for (int32_t k = side; k < used; k += kSide) {
+        // a chunk's share, at most 1, and no 0 by underflow (by_definition)
+        const float2 v = at[k];
+        const float share =
+            __builtin_fmaf(v.y * down_to(v.x, all.x), by, v.y > 0.0f ? 0x1p-149f : 0.0f);
+        o += from[(int64_t)k * (D / 4)] * share;
+    }
     sums[threadIdx.x] = o;
     __syncthreads();
     if (side != 0) return;
 #pragma unroll
     for (int k = 1; k < kSide; k++) o += sums[k * (D / 4) + e];
     if (all.y == 0.0f) o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // no weight at all
-    const float by = all.y == 0.0f ? 0.0f : 1.0f / all.y;
-    const uint32_t w[2] = {to16<DT>(o[0] * by) | (uint32_t)to16<DT>(o[1] * by) << 16,
-                           to16<DT>(o[2] * by) | (uint32_t)to16<DT>(o[3] * by) << 16};
+    const uint32_t w[2] = {to16<DT>(o[0]) | (uint32_t)to16<DT>(o[1]) << 16,
+                           to16<DT>(o[2]) | (uint32_t)to16<DT>(o[3]) << 16};
     __builtin_memcpy(__builtin_assume_aligned(out + row * D + 4 * e, 8), w, 8);
 }
 
