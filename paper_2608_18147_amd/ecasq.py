@@ -445,7 +445,8 @@ def ecasq_solve_batched(x, s, bits_per_entry, options=None, stream=None):
 # ---------------------------------------------------------------------------
 # Serving: products with 4-bit weights and the paged key/value cache.  These calls
 # run on their tensors' device, on its current stream or on `stream`, and allocate
-# what they return and their workspace there with torch's allocator.
+# what they return and their workspace there with torch's allocator.  They have no
+# gradients, and refuse tensors that require one where torch records them.
 
 _HALF = {torch.float16: 1, torch.bfloat16: 2}
 
@@ -490,6 +491,12 @@ def _tensor(x, name, dtype, device, shape=None):
     if not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return x
+
+
+def _no_gradient(x, name):
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and there is none: detach it, or call "
+                         "under torch.no_grad()")
 
 
 def _half_tensor(x, name):
@@ -537,6 +544,8 @@ def ecasq_weights_pack(symbols, codebook, scales, group, stream=None):
         raise ValueError("sizes or group out of range")
     if tuple(scales.shape) != (n_out, -(-n_in // group)):
         raise ValueError("scales must be [n_out, ceil(n_in / group)]")
+    _no_gradient(scales, "scales")
+    _no_gradient(codebook, "codebook")
     return _run(_pack, scales.device, stream, symbols, codebook, scales, group, size)
 
 
@@ -558,6 +567,7 @@ def ecasq_matvec(w, x, out=None, stream=None):
     shape = x.shape
     if not shape or shape[-1] != w.n_in:
         raise ValueError(f"x must end in {w.n_in} entries")
+    _no_gradient(x, "x")
     if out is not None:
         _tensor(out, "out", w.dtype, w.device, shape[:-1] + (w.n_out,))
     return _run(_matvec, w.device, stream, w, x, shape, out)
@@ -612,6 +622,9 @@ class ecasq_kv_cache:
         if self.coded:
             for name, x in (("k_books", k_books), ("v_books", v_books)):
                 _tensor(x, name, self.dtype, dev, k.shape[:3] + (16,))
+        for name, x in (("k", k), ("v", v), ("k_books", k_books), ("v_books", v_books)):
+            if x is not None:
+                _no_gradient(x, name)
         self._slots_shape = (self.batch, self.heads, self.slots)
         if mass is not None:
             _tensor(mass, "mass", torch.float32, dev, self._slots_shape)
@@ -658,6 +671,7 @@ def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=
             raise TypeError(f"{name} must be a {kv.dtype} tensor on {dev}")
         if x.dim() != 3 or x.shape[1:] != (kv.heads, kv.head_dim) or x.shape[0] != k.shape[0]:
             raise ValueError(f"{name} must be [rows, {kv.heads}, {kv.head_dim}]")
+        _no_gradient(x, name)
     rows = k.shape[0]
     _tensor(starts, "starts", torch.int32, dev, (kv.batch + 1,))
     if positions is not None:
@@ -704,6 +718,7 @@ def ecasq_kv_attention(kv, q, scale=None, mass_out=None, out=None, stream=None):
         raise TypeError(f"q must be a {kv.dtype} tensor on {kv.device}")
     if q.dim() != 3 or q.shape[0] != kv.batch or q.shape[2] != kv.head_dim:
         raise ValueError(f"q must be [{kv.batch}, q_heads, {kv.head_dim}]")
+    _no_gradient(q, "q")
     if mass_out is not None:
         _tensor(mass_out, "mass_out", torch.float32, kv.device, kv._slots_shape)
     if out is not None:
