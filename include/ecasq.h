@@ -396,7 +396,7 @@ ecasq_status ecasq_solve_batched(const void *x, ecasq_dtype dt, int64_t n, int64
  * against packed_bytes), 16-byte aligned.
  * ecasq_matvec: x, device, m rows of n_in entries x_stride >= n_in entries
  * apart, 1 <= m <= 2^20; y, device, m x n_out, outside the range from x's first
- * entry to its last.  x and y need the alignment of their type only.  The packed
+ * entry to its last and outside the packed matrix (else ECASQ_EINVAL).  x and y need the alignment of their type only.  The packed
  * matrix is read once for every 16 rows of x.  No workspace; results do not depend
  * on the run or on m's other rows.  Both return once the work is enqueued.
  */
@@ -469,7 +469,9 @@ typedef struct {
  * outside 1 .. 16 (0 marks a row with NaN or Inf) is stored as NaN.  k_hat, v_hat
  * (device, rows x heads x head_dim of dt, both or neither) receive the rows as
  * they will be read, so that a prompt can be computed with them; rows that are
- * left out are not written.  For coded = 0 the last eight arguments are ignored
+ * left out are not written.  k_hat may be new_k and v_hat new_v where the rows lie one after the
+ * other; otherwise neither may meet the other, or the range from the first to the last entry of
+ * new_k or new_v (else ECASQ_EINVAL).  For coded = 0 the last eight arguments are ignored
  * but for k_hat and v_hat, which must be NULL.  Returns once the work is
  * enqueued.
  */
@@ -497,8 +499,8 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  * takes many times as long.
  * mass_out (device, as c->mass; NULL: no weights): for each slot below lens[b]
  * and head g, c->mass (0 where that is NULL) plus p_t summed over g's query heads
- * in order; slots past lens[b] are left as they are.  mass_out may be c->mass; with
- * it batch heads max_pages page_size is at most 2^30.
+ * in order; slots past lens[b] are left as they are.  mass_out may be c->mass, but not lie
+ * over a part of it (ECASQ_EINVAL); with it batch heads max_pages page_size is at most 2^30.
  * The length is split over workgroups and joined where batch and heads alone do
  * not fill the card; results are the same bit for bit from run to run.
  * workspace: at least ecasq_kv_attention_workspace bytes (0 for a bad cache or
@@ -520,7 +522,8 @@ ecasq_status ecasq_kv_attention(const ecasq_kv_cache *c, const void *q, int64_t 
  * are, and slots at or above keep may be given to another sequence after the
  * call.  mass_out, pos_out (as c->mass and c->pos, which are needed) receive the
  * slots below min(lens[b], keep), lens_out (batch) that number; they may be
- * c->mass, c->pos and c->lens.  keep >= 1, 0 <= recent <= keep, and batch heads
+ * c->mass, c->pos and c->lens, but not lie over a part of those or over each other
+ * (ECASQ_EINVAL).  keep >= 1, 0 <= recent <= keep, and batch heads
  * max_pages page_size at most 2^30.  Slots without a page are ranked and moved like
  * others but have no rows (a row moved from one leaves the freed slot's row as it was).
  * workspace: ecasq_kv_evict_workspace bytes (0 for a bad cache or keep), 256-byte

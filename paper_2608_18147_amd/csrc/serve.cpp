@@ -49,10 +49,25 @@ bool slots_ok(const ecasq_kv_cache* c) {
     return (int64_t)c->batch * c->heads * kv_slots(*c) <= ((int64_t)1 << 30);
 }
 
+// Do na bytes at a meet nb at b?
+bool meet(const void* a, size_t na, const void* b, size_t nb) {
+    const auto a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    return a0 < b0 + nb && b0 < a0 + na;
+}
+
 // Do `rows` rows of `row` 16-bit entries, a_stride apart at a, meet n at b?
 bool overlap(const void* a, int64_t rows, int64_t row, int64_t a_stride, const void* b, int64_t n) {
-    const auto a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return a0 < b0 + 2 * (uintptr_t)n && b0 < a0 + 2 * ((uintptr_t)(rows - 1) * a_stride + row);
+    return meet(a, 2 * ((size_t)(rows - 1) * a_stride + row), b, 2 * (size_t)n);
+}
+
+// Does a result of n bytes lie partly over its operand (NULL: there is none)?  It may be the
+// operand itself.
+bool partly(const void* result, const void* operand, size_t n) {
+    return operand && result != operand && meet(result, n, operand, n);
+}
+
+size_t slots_bytes(const ecasq_kv_cache* c) {
+    return 4 * (size_t)c->batch * c->heads * (size_t)kv_slots(*c);
 }
 
 ecasq_status status(hipError_t e) { return e == hipSuccess ? ECASQ_OK : ECASQ_EHIP; }
@@ -87,8 +102,10 @@ ecasq_status ecasq_matvec(const void* packed, ecasq_dtype dt, int64_t n_out, int
         x_stride < n_in || x_stride > ((int64_t)1 << 40) ||
         overlap(x, m, n_in, x_stride, y, m * n_out))
         return ECASQ_EINVAL;
-    return status(launch_matvec(static_cast<const char*>(packed), dt, Weights{n_out, n_in, group},
-                                x, m, x_stride, y, static_cast<hipStream_t>(stream)));
+    const Weights w{n_out, n_in, group};
+    if (meet(packed, (size_t)w.bytes(), y, 2 * (size_t)(m * n_out))) return ECASQ_EINVAL;
+    return status(launch_matvec(static_cast<const char*>(packed), dt, w, x, m, x_stride, y,
+                                static_cast<hipStream_t>(stream)));
 }
 
 ecasq_status ecasq_kv_write(const ecasq_kv_cache* c, const void* new_k, int64_t k_stride,
@@ -114,6 +131,15 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache* c, const void* new_k, int64_t 
     if (c->coded) {
         if (!k_codebooks || !k_counts || !v_codebooks || !v_counts || s < 2 || s > 32 ||
             (k_hat == nullptr) != (v_hat == nullptr) || !aligned(k_hat, 2) || !aligned(v_hat, 2))
+            return ECASQ_EINVAL;
+        const int64_t all = rows * row;
+        if (k_hat && (overlap(k_hat, 1, all, all, v_hat, all) ||
+                      overlap(new_v, rows, row, v_stride, k_hat, all) ||
+                      overlap(new_k, rows, row, k_stride, v_hat, all) ||
+                      (overlap(new_k, rows, row, k_stride, k_hat, all) &&
+                       (k_hat != new_k || k_stride != row)) ||
+                      (overlap(new_v, rows, row, v_stride, v_hat, all) &&
+                       (v_hat != new_v || v_stride != row))))
             return ECASQ_EINVAL;
         n.k_books = k_codebooks;
         n.v_books = v_codebooks;
@@ -146,6 +172,7 @@ ecasq_status ecasq_kv_attention(const ecasq_kv_cache* c, const void* q, int64_t 
         return ECASQ_EWORKSPACE;
     const int64_t row = (int64_t)q_heads * c->head_dim;
     if (overlap(q, c->batch, row, q_stride, out, c->batch * row)) return ECASQ_EINVAL;
+    if (mass_out && partly(mass_out, c->mass, slots_bytes(c))) return ECASQ_EINVAL;
     return status(launch_kv_attention(*c, q, q_stride, q_heads, (float)scale, mass_out, out,
                                       static_cast<char*>(workspace),
                                       static_cast<hipStream_t>(stream)));
@@ -164,6 +191,11 @@ ecasq_status ecasq_kv_evict(const ecasq_kv_cache* c, int32_t keep, int32_t recen
         return ECASQ_EINVAL;
     if (!workspace || !aligned(workspace, 256)) return ECASQ_EINVAL;
     if (workspace_bytes < kv_evict_bytes(*c, keep)) return ECASQ_EWORKSPACE;
+    const size_t n = slots_bytes(c);
+    if (partly(mass_out, c->mass, n) || partly(pos_out, c->pos, n) || meet(mass_out, n, pos_out, n) ||
+        meet(mass_out, n, c->pos, n) || meet(pos_out, n, c->mass, n) ||
+        partly(lens_out, c->lens, 4 * (size_t)c->batch))
+        return ECASQ_EINVAL;
     return status(launch_kv_evict(*c, keep, recent, mass_out, pos_out, lens_out,
                                   static_cast<char*>(workspace),
                                   static_cast<hipStream_t>(stream)));

@@ -1,0 +1,94 @@
+"""Results of the serving operators over their operands: refused where a part of an operand would be
+written before it is read, taken where a result is the operand itself."""
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_18147_amd import ecasq
+
+FAKE = 0x100000000  # aligned, never read: every call that has no GPU is refused on the host
+
+
+def _cache(**kw):
+    c = ecasq._kv_struct(1, 0, 2, 128, 16, 3, 4, 9, FAKE, FAKE, None, None, FAKE, FAKE, FAKE,
+                         2 * FAKE)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return ctypes.byref(c), 4 * 3 * 2 * 64  # and the bytes of mass or pos
+
+
+def test_products_over_the_packed_matrix_refused():
+    L = ecasq.lib()
+    size = L.ecasq_weights_size(20, 200, 64)
+    for y in (FAKE, FAKE + size - 2, FAKE - 2 * 3 * 20 + 2):
+        assert L.ecasq_matvec(FAKE, 1, 20, 200, 64, 3 * FAKE, 3, 200, None, y) == ecasq.ECASQ_EINVAL
+
+
+def test_weights_over_a_part_of_the_mass_refused():
+    L, (r, n) = ecasq.lib(), _cache()
+    size = L.ecasq_kv_attention_workspace(r, 4, 1)
+    for at in (4, n - 4, -4, 4 - n):
+        assert L.ecasq_kv_attention(r, 5 * FAKE, 512, 4, 0.1, FAKE + at, None, 6 * FAKE, 7 * FAKE,
+                                    size) == ecasq.ECASQ_EINVAL
+
+
+def test_evictions_over_parts_refused():
+    L, (r, n) = ecasq.lib(), _cache(lens=4 * FAKE)
+    size = L.ecasq_kv_evict_workspace(r, 8)
+    mass, pos, lens, m, p = FAKE, 2 * FAKE, 4 * FAKE, 5 * FAKE, 6 * FAKE
+    for outs in ((mass + 4, p, lens), (mass - n + 4, p, lens), (m, pos + 4, lens), (m, pos + n - 4, lens),
+                 (m, p, lens + 4), (m, p, lens - 8), (m, m, lens), (m, m + n - 4, lens),
+                 (pos, p, lens), (m, mass, lens), (pos, mass, lens)):
+        assert L.ecasq_kv_evict(r, 8, 2, *outs, None, 7 * FAKE, size) == ecasq.ECASQ_EINVAL, outs
+
+
+def test_rounded_rows_over_others_refused():
+    L = ecasq.lib()
+    r, _ = _cache(coded=1, k_books=FAKE, v_books=FAKE)
+    rows, row = 3, 256
+    n = 2 * rows * row
+    k, v, a, b = 10 * FAKE, 11 * FAKE, 12 * FAKE, 13 * FAKE
+    for (kk, ks, vv, vs), hats in (
+            ((k, row, v, row), (k + 2, b)), ((k, row, v, row), (k - n + 2, b)),
+            ((k, row, v, row), (a, v + n - 2)), ((k, row, v, row), (a, a)),
+            ((k, row, v, row), (a, a + n - 2)), ((k, row, v, row), (v, b)),
+            ((k, row, v, row), (a, k)), ((k, row, k, row), (k, b)), ((k, row, k, row), (a, k)),
+            ((k, row + 2, v, row), (k, b)), ((k, row, v, 2 * row), (a, v)),
+            ((k, 2 * row, v, row), (k + 2 * row, b))):
+        assert L.ecasq_kv_write(r, kk, ks, vv, vs, rows, FAKE, None, None, FAKE, FAKE, FAKE, FAKE, 16,
+                                0, *hats) == ecasq.ECASQ_EINVAL, (kk, ks, vv, vs, hats)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads", [(64, 3), (128, 2), (256, 5)])
+def test_rows_rounded_in_place(dim, heads):
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    rows, dtype = 40, torch.float16
+    g = torch.Generator().manual_seed(dim)
+    k, v = [torch.randn(rows, heads, dim, generator=g).to(dtype).cuda() for _ in range(2)]
+    books = torch.linspace(-3, 3, 16, dtype=torch.float64).repeat(rows * heads, 1).cuda()
+    t = torch.full((rows * heads,), 16, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+
+    def write(k, v, k_hat, v_hat):
+        kv = ecasq.ecasq_kv_cache(
+            *[torch.zeros(3, heads, 16, dim // 2, dtype=torch.uint8, device="cuda") for _ in "kv"],
+            torch.arange(3, dtype=torch.int32, device="cuda").reshape(1, 3),
+            torch.tensor([rows], dtype=torch.int32, device="cuda"),
+            *[torch.zeros(3, heads, 16, 16, dtype=dtype, device="cuda") for _ in "kv"])
+        ecasq.ecasq_kv_write(kv, k, v, starts, k_codebooks=books, k_counts=t, v_codebooks=books,
+                             v_counts=t, seed=1, k_hat=k_hat, v_hat=v_hat)
+        return kv
+
+    k_hat, v_hat = torch.zeros_like(k), torch.zeros_like(v)
+    want = write(k, v, k_hat, v_hat)
+    k2, v2 = k.clone(), v.clone()
+    got = write(k2, v2, k2, v2)
+    assert torch.equal(k2, k_hat) and torch.equal(v2, v_hat)
+    for name in ("k", "v", "k_books", "v_books"):
+        assert torch.equal(getattr(got, name), getattr(want, name))
+    with pytest.raises(ecasq.EcasqError):
+        write(k, v, v, k_hat)
