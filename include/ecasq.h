@@ -457,7 +457,9 @@ typedef struct {
  * new_k, new_v: device, `rows` (1 to 2^23) tokens of heads x head_dim entries of dt,
  * k_stride and v_stride (>= heads head_dim) entries apart, of their type's alignment.
  * With c->mass, the slot's weight becomes 0; with c->pos, its position becomes
- * positions[i], or the slot itself where positions is NULL.
+ * positions[i], or the slot itself where positions is NULL.  The slot is the token's place in
+ * its sequence only until ecasq_kv_evict has cut that one: from then on positions has to be
+ * given, or new tokens count as no newer than the slots that they are put into.
  *
  * A coded cache takes each row's codebook as ecasq_solve_batched returns it for
  * the rows of the same tokens (row r = token heads + head): k_codebooks, device,

@@ -662,7 +662,9 @@ def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=
                    v_codebooks=None, v_counts=None, seed=0, k_hat=None, v_hat=None, stream=None):
     """Writes new tokens' rows k, v [rows, heads, head_dim] into the cache, rows
     starts[b] .. starts[b+1]-1 (int32, device) at the end of sequence b, whose lens
-    already counts them.  A cache of symbols takes the rows' codebooks and counts
+    already counts them.  positions (int32 [rows], device) are the tokens' places in their
+    sequences; without them the slots count as such, which holds until a sequence
+    has been cut by ecasq_kv_evict.  A cache of symbols takes the rows' codebooks and counts
     as ecasq_solve_batched returns them for k.reshape(rows * heads, head_dim), and
     gives back the rounded rows in k_hat, v_hat where they are given."""
     dev = kv.device
