@@ -467,7 +467,9 @@ typedef struct {
  * most 16; the same for v.  The values are rounded to dt (they are exact where
  * the codebook was solved on rows of dt) and entry e = r head_dim + j is
  * rounded as ecasq_quantize rounds, its uniform from counter (h mod 2^32, h /
- * 2^32, w, 0), h = e / 2, w = 2 for keys and 3 for values.  A row with a count
+ * 2^32, w, 0), h = e / 2, w = 2 for keys and 3 for values.  Rows are counted from 0 in every
+ * call: calls whose roundings are to be independent (a model's layers, its steps) need a
+ * seed each.  A row with a count
  * outside 1 .. 16 (0 marks a row with NaN or Inf) is stored as NaN.  k_hat, v_hat
  * (device, rows x heads x head_dim of dt, both or neither) receive the rows as
  * they will be read, so that a prompt can be computed with them; rows that are

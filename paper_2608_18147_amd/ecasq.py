@@ -666,7 +666,8 @@ def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=
     sequences; without them the slots count as such, which holds until a sequence
     has been cut by ecasq_kv_evict.  A cache of symbols takes the rows' codebooks and counts
     as ecasq_solve_batched returns them for k.reshape(rows * heads, head_dim), and
-    gives back the rounded rows in k_hat, v_hat where they are given."""
+    gives back the rounded rows in k_hat, v_hat where they are given.  Calls with one seed
+    draw the same uniforms: every layer and step needs its own."""
     dev = kv.device
     for name, x in (("k", k), ("v", v)):
         if not isinstance(x, torch.Tensor) or x.dtype != kv.dtype or x.device != dev:
