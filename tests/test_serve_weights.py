@@ -1,0 +1,222 @@
+"""Attention's weights as they enter the second product, and the chunks that are joined, by a
+bound that an error of one 16-bit rounding of the weights, or a chunk that is missing, would
+pass.
+
+Keys are multiples of 1/4 up to 2 and queries of 1 and -1: scores are exact sums.  With z a score in
+powers of two, Z the largest |z|, u = 2^-24 the relative rounding of fp32:
+  the exponent   z's factor (scale, its product with log2 e, the constant) 4 u Z, the maximum (and,
+                 in f16, 7 off it) and the difference u (Z + 7) + u (2 Z + 7): u (7 Z + 14) in all,
+                 times ln 2 for the weight, and 2 u for the exponential (1 ulp): dw
+  two parts      bf16: half a step of a remainder of half a step, 2^-16; f16: toward zero twice,
+                 2^-20, and half of the smallest step, 2^-25, against weights of 2^7 and more
+                 for the largest: 2^-31 of sum |V|
+  sums           a wavefront adds 32 slots at a time and of four wavefronts' slots every fourth
+                 32, two products a time, each of 32 terms and the sum so far, which may all
+                 round (f = 2 u each): 66 f a round; 8 roundings a round for the sum of
+                 the weights, then 12 for lanes, wavefronts and the quotient; parts of chunks: one a
+                 chunk at most
+(a wavefront's rounds are at most those of a workgroup that takes the whole sequence,
+slots / 128), so that |out - want| <= e |want| + (2 dw + parts + sums) sum p |V|, e the result's own rounding.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import serve
+from paper_2608_18147_amd import ecasq
+
+U = 2.0 ** -24
+TYPES = [torch.float16, torch.bfloat16]
+
+
+def _centred_case(lens, heads, group, dim, page, dtype, coded, seed, scale):
+    """A cache (its arrays) and queries whose scores are exact, with values whose weighted mean
+    is near 0 for every query head of a group (which share one query): an error of the weights
+    then shows beside a result that has next to no rounding of its own.  Coded rows of a
+    sequence's head have the same symbols, and each of the 16 values is centred over the slots."""
+    g = torch.Generator().manual_seed(seed)
+    c, pages = {}, [-(-n // page) for n in lens]
+    n_pages, width = sum(pages) + 1, max(pages)
+    order = torch.randperm(n_pages, generator=g).to(torch.int32)
+    c["table"] = torch.full((len(lens), width), -1, dtype=torch.int32)
+    for b, k in enumerate(pages):
+        c["table"][b, :k] = order[sum(pages[:b]):sum(pages[:b]) + k]
+    shape = (n_pages, heads, page)
+    if coded:
+        c["k"] = torch.randint(0, 256, shape + (dim // 2,), generator=g, dtype=torch.uint8)
+        c["k_books"] = ((torch.arange(16) - 8) / 4).expand(shape + (16,)).contiguous().to(dtype)
+        c["v"], name, m = torch.zeros(shape + (dim // 2,), dtype=torch.uint8), "v_books", 16
+    else:
+        c["k"] = (torch.randint(-8, 9, shape + (dim,), generator=g) / 4).to(dtype)
+        name, m = "v", dim
+    c[name] = torch.full(shape + (m,), float("nan")).to(dtype)
+    c["lens"] = torch.tensor(lens, dtype=torch.int32)
+    q = (torch.randint(0, 2, (len(lens), heads, 1, dim), generator=g) * 2 - 1).to(dtype)
+    q = q.expand(-1, -1, group, -1).reshape(len(lens), heads * group, dim).contiguous()
+    o = _arrays(c)
+    for b, n in enumerate(lens):
+        at = c["table"][b, : pages[b]].long()
+        for h in range(heads):
+            k = torch.from_numpy(serve._rows(o, "k", b, h, list(range(n))))
+            p = torch.softmax(scale * (k @ q[b, h * group].double()), 0)
+            v = torch.randn((n, m), generator=g, dtype=torch.float64)
+            full = torch.full((pages[b] * page, m), float("nan"), dtype=torch.float64)
+            full[:n] = v - p @ v
+            c[name][at, h] = full.reshape(pages[b], page, m).to(dtype)
+            if coded:
+                c["v"][at, h] = torch.randint(0, 256, (dim // 2,), generator=g, dtype=torch.uint8)
+    return c, q
+
+
+def _arrays(c):
+    return {k: v.numpy() if v.dtype in (torch.uint8, torch.int32) else v.double().numpy()
+            for k, v in c.items()}
+
+
+def _bound(o, q, scale, dtype, want, absolute):
+    """The bound above for every result, [batch, q_heads, dim]."""
+    half = dtype == torch.float16
+    heads = o["k"].shape[1]
+    tol = np.zeros(want.shape)
+    for b in range(q.shape[0]):
+        n = serve.length(o, b)
+        slots = list(range(n))
+        for h in range(heads):
+            k, v = (serve._rows(o, name, b, h, slots) for name in ("k", "v"))
+            part = slice(h * q.shape[1] // heads, (h + 1) * q.shape[1] // heads)
+            Z = np.abs(scale * 1.4427 * (k @ q[b, part].T)).max()
+            dw = np.log(2) * U * (7 * Z + 14) + 2 * U
+            rounds = -(-n // 128)
+            sums = rounds * (66 * 2 * U + 8 * U) + 12 * U + -(-n // 128) * U
+            split = 2.0 ** -20 if half else 2.0 ** -16
+            tol[b, part] = (2 * dw + split + sums) * absolute[b, part]
+            if half:
+                tol[b, part] += 2.0 ** -31 * np.abs(v).sum(0)
+    e = torch.finfo(dtype).eps / 2
+    return tol + e * np.abs(want) + e * torch.finfo(dtype).tiny
+
+
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+SCALE = 0.1
+SHAPES = [([40, 100], 2, 4, 128, 16), ([128], 1, 1, 64, 32), ([17, 33, 90], 3, 2, 64, 16),
+          ([70, 127], 1, 16, 256, 32)]
+
+
+CASES = pytest.mark.parametrize("lens,heads,group,dim,page,dtype,coded", [
+    s + (d, c) for s in SHAPES for d in TYPES for c in (False, True)])
+
+
+@CASES
+def test_the_bound_sees_weights_rounded_once(lens, heads, group, dim, page, dtype, coded):
+    """Planted in the plain form: weights rounded to 16 bits once do not keep the bound, in two
+    parts they keep it by far."""
+    c, q = _centred_case(lens, heads, group, dim, page, dtype, coded, 5, SCALE)
+    o, qd = _arrays(c), q.double().numpy()
+    want, _, absolute, _ = serve.attention(o, qd, SCALE)
+    tol = _bound(o, qd, SCALE, dtype, want, absolute)
+
+    def toward_zero(x):
+        y = x.to(torch.float16)
+        return torch.where(y.double() > x, (y.view(torch.int16) - 1).view(torch.float16), y).double()
+
+    worst = [0.0, 0.0]
+    for b, n in enumerate(lens):
+        for h in range(heads):
+            k, v = (serve._rows(o, name, b, h, list(range(n))) for name in ("k", "v"))
+            z = SCALE * np.log2(np.e) * (k @ qd[b, h * group])
+            w = torch.from_numpy(np.exp2(z - z.max() + 7))
+            if dtype == torch.float16:
+                first = toward_zero(w)
+                both = first + toward_zero(w - first)
+            else:
+                first = w.to(dtype).double()
+                both = first + (w - first).to(dtype).double()
+            for i, x in enumerate((first, both)):
+                got = (x / w.sum()).numpy() @ v
+                worst[i] = max(worst[i], (np.abs(got - want[b, h * group]) / tol[b, h * group]).max())
+    print(worst)
+    assert worst[0] > 2 and worst[1] < 0.3, worst
+
+
+@pytest.mark.gpu
+@CASES
+def test_weights_in_two_parts(lens, heads, group, dim, page, dtype, coded):
+    _need_gpu()
+    print("[case] weights", lens, heads, group, dim, dtype, coded, flush=True)
+    c, q = _centred_case(lens, heads, group, dim, page, dtype, coded, 5, SCALE)
+    o, qd = _arrays(c), q.double().numpy()
+    want, _, absolute, _ = serve.attention(o, qd, SCALE)
+    tol = _bound(o, qd, SCALE, dtype, want, absolute)
+    kv = ecasq.ecasq_kv_cache(**{k: v.cuda() for k, v in c.items()})
+    out = ecasq.ecasq_kv_attention(kv, q.cuda(), scale=SCALE).double().cpu().numpy()
+    worst = (np.abs(out - want) / tol).max()
+    print("of the bound:", worst, flush=True)
+    assert worst <= 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,heads,group,dim,page", [
+    ([40001, 129, 700], 2, 3, 128, 64), ([1500, 2611], 1, 17, 64, 16), ([20000], 1, 2, 256, 32),
+    ([9000, 0, 300, 8999], 3, 1, 128, 128)])
+def test_every_block_of_a_split_sequence_counts(lens, heads, group, dim, page, dtype, coded):
+    """Entry d of slot s is 1 where s / 64 = d modulo the row's length, else 0: a result is the
+    weight of every dim-th block of 64 slots, and a chunk that is missing, or counted twice or
+    with another's weight, takes or adds a tenth of some results at least."""
+    _need_gpu()
+    print("[case] blocks", lens, heads, group, dim, dtype, coded, flush=True)
+    g = torch.Generator().manual_seed(dim)
+    pages = [-(-n // page) for n in lens]
+    n_pages, width = sum(pages), max(pages)
+    order = torch.randperm(n_pages, generator=g).to(torch.int32)
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    block = torch.zeros(n_pages, page, dtype=torch.long)
+    for b, k in enumerate(pages):
+        table[b, :k] = order[sum(pages[:b]):sum(pages[:b]) + k]
+        block[table[b, :k].long()] = (torch.arange(k * page) // 64 % dim).reshape(k, page)
+    ones = torch.nn.functional.one_hot(block, dim)[:, None].expand(-1, heads, -1, -1)
+    keys = torch.randint(-8, 8, (n_pages, heads, page, dim), generator=g)
+    c = dict(table=table, lens=torch.tensor(lens, dtype=torch.int32))
+    if coded:
+        for name, x in (("k", keys + 8), ("v", 5 * ones)):
+            c[name] = (x[..., 0::2] | x[..., 1::2] << 4).to(torch.uint8)
+        books = torch.zeros(n_pages, heads, page, 16)
+        c["k_books"] = (books + (torch.arange(16) - 8) / 4).to(dtype)
+        books[..., 5] = 1.0
+        c["v_books"] = books.to(dtype)
+    else:
+        c["k"], c["v"] = (keys / 4).to(dtype), ones.contiguous().to(dtype)
+    q = (torch.randint(0, 2, (len(lens), heads * group, dim), generator=g) * 2 - 1).to(dtype)
+    kv = ecasq.ecasq_kv_cache(**{k: v.cuda() for k, v in c.items()},
+                              mass=torch.zeros(len(lens), heads, width * page, device="cuda"))
+    mass = torch.full_like(kv.mass, -1.0)
+    scale = 0.05
+    out = ecasq.ecasq_kv_attention(kv, q.cuda(), scale=scale, mass_out=mass).double().cpu()
+    e = torch.finfo(dtype).eps / 2
+    for b, n in enumerate(lens):
+        at = table[b, : pages[b]].long()
+        for h in range(heads):
+            k = keys[at, h].reshape(-1, dim)[:n].double() / 4
+            part = slice(h * group, (h + 1) * group)
+            z = scale * (q[b, part].double() @ k.T)
+            p = torch.softmax(z, 1)
+            want = torch.zeros(group, dim, dtype=torch.float64)
+            want.index_add_(1, torch.arange(n) // 64 % dim, p)
+            Z = float(z.abs().max()) * 1.4427 if n else 0.0
+            dw = float(np.log(2)) * U * (7 * Z + 14) + 2 * U
+            rounds = n // 128 + 1
+            rest = 2 * dw + 2.0 ** -16 + rounds * (66 * 2 * U + 9 * U) + 12 * U
+            tol = (rest + e) * want + n * 2.0 ** -31 + e * torch.finfo(dtype).tiny
+            assert rest < 0.02  # (far from a tenth)
+            assert torch.all((out[b, part] - want).abs() <= tol), (b, h)
+            # a slot's weight: as above without the second product
+            total = p.sum(0)
+            off = (2 * dw + rounds * 8 * U + (16 + group) * U) * total
+            assert torch.all((mass[b, h, :n].double().cpu() - total).abs() <= off + 1e-38), (b, h)
+        assert torch.all(mass[b, :, n:] == -1.0)
