@@ -1,6 +1,5 @@
 """Attention's weights as they enter the second product, and the chunks that are joined, by a
-bound that an error of one 16-bit rounding of the weights, or a chunk that is missing, would
-pass.
+bound that one 16-bit rounding of the weights, or a chunk that is missing, would break.
 
 Keys are multiples of 1/4 up to 2 and queries of 1 and -1: scores are exact sums.  With z a score in
 powers of two, Z the largest |z|, u = 2^-24 the relative rounding of fp32:
@@ -8,8 +7,8 @@ powers of two, Z the largest |z|, u = 2^-24 the relative rounding of fp32:
                  in f16, 7 off it) and the difference u (Z + 7) + u (2 Z + 7): u (7 Z + 14) in all,
                  times ln 2 for the weight, and 2 u for the exponential (1 ulp): dw
   two parts      bf16: half a step of a remainder of half a step, 2^-16; f16: toward zero twice,
-                 2^-20, and half of the smallest step, 2^-25, against weights of 2^7 and more
-                 for the largest: 2^-31 of sum |V|
+                 2^-20, and a smallest step, 2^-24, against 2^7 and more for the largest
+                 weight: 2^-31 of sum |V|
   sums           a wavefront adds 32 slots at a time and of four wavefronts' slots every fourth
                  32, two products a time, each of 32 terms and the sum so far, which may all
                  round (f = 2 u each): 66 f a round; 8 roundings a round for the sum of
