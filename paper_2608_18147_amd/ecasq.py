@@ -494,6 +494,8 @@ def _tensor(x, name, dtype, device, shape=None):
 
 
 def _no_gradient(x, name):
+    """Refuses x where its gradient would be recorded.  (Calls of each step ask for
+    x.requires_grad themselves.)"""
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, and there is none: detach it, or call "
                          "under torch.no_grad()")
@@ -567,7 +569,8 @@ def ecasq_matvec(w, x, out=None, stream=None):
     shape = x.shape
     if not shape or shape[-1] != w.n_in:
         raise ValueError(f"x must end in {w.n_in} entries")
-    _no_gradient(x, "x")
+    if x.requires_grad:
+        _no_gradient(x, "x")
     if out is not None:
         _tensor(out, "out", w.dtype, w.device, shape[:-1] + (w.n_out,))
     return _run(_matvec, w.device, stream, w, x, shape, out)
@@ -674,7 +677,8 @@ def ecasq_kv_write(kv, k, v, starts, positions=None, k_codebooks=None, k_counts=
             raise TypeError(f"{name} must be a {kv.dtype} tensor on {dev}")
         if x.dim() != 3 or x.shape[1:] != (kv.heads, kv.head_dim) or x.shape[0] != k.shape[0]:
             raise ValueError(f"{name} must be [rows, {kv.heads}, {kv.head_dim}]")
-        _no_gradient(x, name)
+        if x.requires_grad:
+            _no_gradient(x, name)
     rows = k.shape[0]
     _tensor(starts, "starts", torch.int32, dev, (kv.batch + 1,))
     if positions is not None:
@@ -721,7 +725,8 @@ def ecasq_kv_attention(kv, q, scale=None, mass_out=None, out=None, stream=None):
         raise TypeError(f"q must be a {kv.dtype} tensor on {kv.device}")
     if q.dim() != 3 or q.shape[0] != kv.batch or q.shape[2] != kv.head_dim:
         raise ValueError(f"q must be [{kv.batch}, q_heads, {kv.head_dim}]")
-    _no_gradient(q, "q")
+    if q.requires_grad:
+        _no_gradient(q, "q")
     if mass_out is not None:
         _tensor(mass_out, "mass_out", torch.float32, kv.device, kv._slots_shape)
     if out is not None:
