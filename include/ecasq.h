@@ -384,7 +384,9 @@ ecasq_status ecasq_solve_batched(const void *x, ecasq_dtype dt, int64_t n, int64
  *   y[r][o] = sum_g scales[o][g] sum_{i in g} c[symbols[o][i]] x[r][i].
  * The codebook values and the scales are held in dt (ECASQ_F16 or ECASQ_BF16),
  * the type of x and y; products are exact, sums are fp32 (those of up to 128
- * products of one scale first, times the scale, then all), y is rounded once.
+ * products of one scale first, times the scale, then all), y is rounded once.  (What fills a
+ * row up to a multiple of 128 columns is 0 times a finite value of the codebook; with none, rows
+ * of other lengths give NaN.)
  *
  * ecasq_weights_size: bytes of the packed matrix (0 unless 1 <= n_out, n_in <=
  * 2^24, n_out n_in <= 2^40 and group is a positive multiple of 32 up to 2^24; a
@@ -499,8 +501,8 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  * Otherwise a NaN or an infinity in a row that is read reaches the result as the formula says:
  * an infinite value as itself however small its weight is, as NaN where it meets one of the other
  * sign or its score is -inf; what lies in slots past lens[b] does not.  Finite values give finite
- * results.  Where infinities or values near the type's largest are met, a part of the call
- * takes many times as long.
+ * results.  Where NaN, infinities or values near the type's largest are met among the values, a
+ * part of the call takes many times as long.
  * mass_out (device, as c->mass; NULL: no weights): for each slot below lens[b]
  * and head g, c->mass (0 where that is NULL) plus p_t summed over g's query heads
  * in order; slots past lens[b] are left as they are.  mass_out may be c->mass, but not lie
@@ -509,7 +511,8 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  * not fill the card; results are the same bit for bit from run to run.
  * workspace: at least ecasq_kv_attention_workspace bytes (0 for a bad cache or
  * q_heads), 256-byte aligned, its contents of no meaning between calls; calls that
- * overlap need one each.  Returns once the work is enqueued.
+ * overlap need one each.  With mass_out it holds a float for every query head and slot of
+ * the table, in use or not.  Returns once the work is enqueued.
  */
 size_t ecasq_kv_attention_workspace(const ecasq_kv_cache *c, int32_t q_heads, int32_t with_mass);
 ecasq_status ecasq_kv_attention(const ecasq_kv_cache *c, const void *q, int64_t q_stride,

@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256) void k_weights_pack(const uint8_t* __restrict_
 // 8192 columns a wavefront has one chunk and reads its part of x once for all tiles:
 // loads return in order, so a wait for x was one for the symbols behind it (28672 x
 // 8192, one row of x: 41 us against 30).  Above, it has several; the rows of x are then
-// in LDS where they fit (28672 columns for one row, 14336 for two), or a part of x is
+// in LDS where they fit (32256 columns for one row, 15872 for two, 10752 for three), or a part of x is
 // read again for every `turns` tiles (8192 x 28672, one row: 28 us by the first, 32 by the
 // second).
 //
