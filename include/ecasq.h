@@ -398,9 +398,10 @@ ecasq_status ecasq_solve_batched(const void *x, ecasq_dtype dt, int64_t n, int64
  * against packed_bytes), 16-byte aligned.
  * ecasq_matvec: x, device, m rows of n_in entries x_stride >= n_in entries
  * apart, 1 <= m <= 2^20; y, device, m x n_out, outside the range from x's first
- * entry to its last and outside the packed matrix (else ECASQ_EINVAL).  x and y need the alignment of their type only.  The packed
- * matrix is read once for every 16 rows of x.  No workspace; results do not depend
- * on the run or on m's other rows.  Both return once the work is enqueued.
+ * entry to its last and outside the packed matrix (else ECASQ_EINVAL).  x and y need the
+ * alignment of their type only.  The packed matrix is read once for every 16 rows of x.  No
+ * workspace; results do not depend on the run or on m's other rows.  Both return once the work
+ * is enqueued.
  */
 size_t ecasq_weights_size(int64_t n_out, int64_t n_in, int64_t group);
 ecasq_status ecasq_weights_pack(const uint8_t *symbols, const double *codebook, int32_t t,
@@ -500,8 +501,8 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache *c, const void *new_k, int64_t 
  * -inf, gives zeros.
  * Otherwise a NaN or an infinity in a row that is read reaches the result as the formula says:
  * an infinite value as itself however small its weight is, as NaN where it meets one of the other
- * sign or its score is -inf; what lies in slots past lens[b] does not.  Finite values give finite
- * results.  Where NaN, infinities or values near the type's largest are met among the values, a
+ * sign or its score is -inf; what lies in slots past lens[b] does not.  Finite values and scores
+ * give finite results.  Where NaN, infinities or values near the type's largest are met among the values, a
  * part of the call takes many times as long.
  * mass_out (device, as c->mass; NULL: no weights): for each slot below lens[b]
  * and head g, c->mass (0 where that is NULL) plus p_t summed over g's query heads

@@ -132,14 +132,15 @@ ecasq_status ecasq_kv_write(const ecasq_kv_cache* c, const void* new_k, int64_t 
         if (!k_codebooks || !k_counts || !v_codebooks || !v_counts || s < 2 || s > 32 ||
             (k_hat == nullptr) != (v_hat == nullptr) || !aligned(k_hat, 2) || !aligned(v_hat, 2))
             return ECASQ_EINVAL;
+        // (a row's entries are read before they are written; in one place, that is all)
         const int64_t all = rows * row;
+        const bool k_there = k_hat == new_k && (k_stride == row || rows == 1);
+        const bool v_there = v_hat == new_v && (v_stride == row || rows == 1);
         if (k_hat && (overlap(k_hat, 1, all, all, v_hat, all) ||
                       overlap(new_v, rows, row, v_stride, k_hat, all) ||
                       overlap(new_k, rows, row, k_stride, v_hat, all) ||
-                      (overlap(new_k, rows, row, k_stride, k_hat, all) &&
-                       (k_hat != new_k || k_stride != row)) ||
-                      (overlap(new_v, rows, row, v_stride, v_hat, all) &&
-                       (v_hat != new_v || v_stride != row))))
+                      (!k_there && overlap(new_k, rows, row, k_stride, k_hat, all)) ||
+                      (!v_there && overlap(new_v, rows, row, v_stride, v_hat, all))))
             return ECASQ_EINVAL;
         n.k_books = k_codebooks;
         n.v_books = v_codebooks;

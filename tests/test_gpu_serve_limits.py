@@ -106,7 +106,7 @@ def test_the_largest_page(coded):
             d[name] = x.reshape(-1, 1, 64, x.shape[-1])
     d["table"] = torch.full((2, 2048), -1, dtype=torch.int32)
     d["table"][0] = torch.arange(2048)
-    d["table"][1, :1024] = torch.arange(2048, 3072)
+    d["table"][1, :1024] = 2048 + torch.arange(1024)
     assert torch.equal(ecasq.ecasq_kv_attention(on_gpu(d), q.cuda()), out)
     ecasq.ecasq_kv_evict(kv, 40000, 100)
     mass, pos, lens, moves = serve.evict({k: _np(v) if v.is_floating_point() else v.numpy()

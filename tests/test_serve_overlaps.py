@@ -79,8 +79,9 @@ def test_rows_rounded_in_place(dim, heads):
             torch.arange(3, dtype=torch.int32, device="cuda").reshape(1, 3),
             torch.tensor([rows], dtype=torch.int32, device="cuda"),
             *[torch.zeros(3, heads, 16, 16, dtype=dtype, device="cuda") for _ in "kv"])
-        ecasq.ecasq_kv_write(kv, k, v, starts, k_codebooks=books, k_counts=t, v_codebooks=books,
-                             v_counts=t, seed=1, k_hat=k_hat, v_hat=v_hat)
+        n = k.shape[0] * heads
+        ecasq.ecasq_kv_write(kv, k, v, starts, k_codebooks=books[:n], k_counts=t[:n],
+                             v_codebooks=books[:n], v_counts=t[:n], seed=1, k_hat=k_hat, v_hat=v_hat)
         return kv
 
     k_hat, v_hat = torch.zeros_like(k), torch.zeros_like(v)
@@ -92,3 +93,14 @@ def test_rows_rounded_in_place(dim, heads):
         assert torch.equal(getattr(got, name), getattr(want, name))
     with pytest.raises(ecasq.EcasqError):
         write(k, v, v, k_hat)
+    # one row, whose distance to the next does not matter
+    one = [x[:1].clone() for x in (k, v)]
+    before = [x.data_ptr() for x in one]
+    kv = write(k[:1].clone(), v[:1].clone(), torch.zeros_like(one[0]), torch.zeros_like(one[1]))
+    starts[1], row = 1, heads * dim
+    kv.lens.fill_(1)
+    assert ecasq.lib().ecasq_kv_write(
+        kv._ref, before[0], 2 * row, before[1], 3 * row, 1, starts.data_ptr(), None,
+        torch.cuda.current_stream().cuda_stream, books.data_ptr(), t.data_ptr(), books.data_ptr(),
+        t.data_ptr(), 16, 1, before[0], before[1]) == 0
+    assert torch.equal(one[0], k_hat[:1]) and torch.equal(one[1], v_hat[:1])
