@@ -87,7 +87,7 @@ __device__ __forceinline__ float float_not_above(double q) {
 // below 2^-20 (one entry in 2^19, or NaN) takes the 64-bit division (4000 tokens of 8 heads of
 // 128: 50 us with 64-bit comparisons, 30 so).  Of the 30 us the generator is 5, the bracket
 // search 2.4 and the books' preparation, by 16 lanes of 64 where a row is 128 entries or more,
-// 2.4; without generator and search 23.6 remain, of 183 instructions a unit 120 or so.
+// 2.4; without generator and search 23.6 remain.
 template <int DT, int D>
 __global__ __launch_bounds__(kWT) void k_kv_round(ecasq_kv_cache c, KvNew n) {
     constexpr int kRows = D < 128 ? 128 / D : 1, kParts = D < 128 ? 1 : D / 128;
